@@ -562,6 +562,173 @@ size_t mipgemm_workspace_size(int64_t m, int64_t n, int64_t k,
 size_t mipgemm_workspace_size_f32(int64_t m, int64_t n, int64_t k,
                                   int orderA, int orderB, int orderC);
 
+/* types of real numbers (x_type, c_type, type) */
+#define MIPGEMM_F32 0
+#define MIPGEMM_BF16 1
+#define MIPGEMM_F16 2
+
+/* activations of mipgemm_s8s8_linear */
+#define MIPGEMM_NONE 0
+#define MIPGEMM_RELU 1
+#define MIPGEMM_GELU 2      /* y Phi(y), Phi the normal distribution function */
+#define MIPGEMM_GELU_TANH 3 /* y (1 + tanh(sqrt(2 / pi) (y + 0.044715 y^3))) / 2 */
+#define MIPGEMM_SILU 4      /* y / (1 + exp(-y)) */
+
+/*
+ * Rows of real numbers brought to 8 bits, a scale to each (the paper's X ~ s_X X^q, Section
+ * 7.3, with s_X by row and taken from the row itself): what the activations of a linear layer
+ * go through on their way to mipgemm_s8s8_linear.
+ *     z(i,j) = X(i,j) norm_weight(j),   a(i) = max over j of |z(i,j)|
+ *     Q(i,j) = rint(127 z(i,j) / a(i)), ties to even
+ *     scales(i) = a(i) / 127, times 1 / sqrt(mean over j of X(i,j)^2 + eps)
+ * norm_weight (DEVICE, `cols` float32) makes it an RMS norm and its quantisation in one pass;
+ * NULL: no norm, the weights are ones and the factor of the root is left out (`eps` is not
+ * used).  z and the scale are formed in float32, the squares are summed in float32, the
+ * quotient is correctly rounded, so that Q does not depend on the order of any sum.  A row of
+ * zeros gets codes and a scale of zero; a row with an infinity or NaN in z codes of zero and
+ * a NaN as its scale, so that what is computed from it is NaN.  X is row-major of x_type with
+ * rows ldx elements apart, Q row-major int8 with rows ldq apart; scales holds `rows` float32.
+ * Nothing needs more alignment than its type's.  Argument numbers: rows=1 cols=2 X=3 ldx=4
+ * x_type=5 norm_weight=6 eps=7 (finite, not negative) Q=8 ldq=9 scales=10 stream=11.
+ */
+int mipgemm_quantize_rows(int64_t rows, int64_t cols,
+                          const void *X, int64_t ldx, int x_type,
+                          const float *norm_weight, float eps,
+                          int8_t *Q, int64_t ldq, float *scales,
+                          void *stream);
+
+/*
+ * A linear layer on 8-bit operands: the product of mipgemm_s8s8s32 with scales, bias,
+ * activation and residual in its write-back,
+ *     C(i,j) = act( float(S(i,j)) a_scales(i) b_scales(j) + bias(j) ) + R(i,j)
+ * with S the int32 sum (wrapping modulo 2^32), completed in integers before anything is
+ * converted, everything behind it in float32 and one rounding to the type of C.  A is m x k
+ * row-major; B is k x n in either order (weights stored n x k, as layers keep them, are
+ * MIPGEMM_COL_MAJOR); C and R are m x n row-major of c_type.  a_scales (m float32), b_scales and
+ * bias (n float32) and R may each be NULL: 1, 1, 0 and 0.  R may be C itself (the same
+ * pointer and leading dimension): a residual added in place; otherwise they must not overlap.
+ * The workspace is optional as in the f32 entry points and as large
+ * (mipgemm_workspace_size_f32): operands that cannot be streamed are packed into it, and a
+ * product with few tiles splits k only with room for slots of partial sums.  The result is
+ * the same bits with and without it.
+ * Argument numbers: m=1 n=2 k=3 A=4 lda=5 a_scales=6 B=7 ldb=8 orderB=9 b_scales=10 bias=11
+ * activation=12 R=13 ldr=14 C=15 ldc=16 c_type=17 workspace=18 workspace_bytes=19 stream=20.
+ */
+int mipgemm_s8s8_linear(int64_t m, int64_t n, int64_t k,
+                        const int8_t *A, int64_t lda, const float *a_scales,
+                        const int8_t *B, int64_t ldb, int orderB, const float *b_scales,
+                        const float *bias, int activation,
+                        const void *R, int64_t ldr,
+                        void *C, int64_t ldc, int c_type,
+                        void *workspace, size_t workspace_bytes,
+                        void *stream);
+
+/*
+ * The cache of keys and values in 4 bits.  32 channels of one token and head are a group,
+ * x ~ s (n - z) with n in 0 .. 15, z in -127 .. 127 and s a float16 of 4 significant bits:
+ *     s = max((max - min) / 15, max |x| / 112), rounded up to such a number (to a multiple of
+ *         2^-17 below 2^-14)
+ *     z = -rint(min / s),  n = min(max(rint(x / s) + z, 0), 15)
+ * 4.5 bits a channel; zero is a value of every group; s (n - z) is exact in float16.  |x| is cut
+ * at 57344 first; a group with an infinity or NaN reads back as NaN.
+ *
+ * The cache is `pages` pages of page_tokens tokens (a power of two, 16 to 1024) of kv_heads heads
+ * of head_dim channels (64, 128 or 256): DEVICE memory of mipgemm_kv4_bytes bytes (0 for
+ * invalid sizes), 16-byte aligned, owned by the caller; it needs no clearing, since nothing is
+ * read that was not written.  Slot p * page_tokens + t is token t of page p.  A page holds, for
+ * one head after the other, the keys' codes (page_tokens x head_dim / 2 bytes; channel 8 w + e is
+ * nibble e, from the lowest on, of a token's word w), the keys' pairs (head_dim / 32 groups x
+ * page_tokens x 2 bytes: the bits of s above its lowest seven, then z), the values' codes (the same
+ * words with four tokens interleaved: word w of token t at byte
+ * 16 ((t / 4) (head_dim / 8) + w) + 4 (t % 4)) and the values' pairs.
+ */
+size_t mipgemm_kv4_bytes(int64_t pages, int64_t page_tokens, int64_t kv_heads, int64_t head_dim);
+
+/* how mipgemm_qk_norm_rope pairs the channels it rotates */
+#define MIPGEMM_ROTATE_HALVES 0 /* j with j + rot_dim / 2 */
+#define MIPGEMM_ROTATE_PAIRS 1  /* 2 j with 2 j + 1 */
+
+/*
+ * Between the projections of an attention layer and the attention: RMS norm of every head of
+ * queries and keys, their rotation by position, and keys and values into the 4-bit cache, in
+ * one pass.  For each token and head of queries (keys with k_weight)
+ *     y(c) = x(c) q_weight(c) / sqrt(mean over c of x(c)^2 + eps)        (q_weight NULL: y = x)
+ *     (y(a), y(b)) <- (y(a) cos - y(b) sin, y(b) cos + y(a) sin)
+ * for the pairs (a, b) = (j, j + rot_dim / 2) or (2 j, 2 j + 1), j < rot_dim / 2 (rot_dim even, 0
+ * to head_dim; 0: no rotation), with cos and sin = cosine, sine(positions(token), j), two
+ * DEVICE tables of table_rows x rot_dim / 2 float32; channels from rot_dim on stay as they are.
+ * Values pass unchanged.  Q, K and V hold a token's heads next to each other, head_dim
+ * channels each, tokens ldq, ldk, ldv elements apart (parts of one matrix of all three, for
+ * example); weights are head_dim float32.  Queries go to Qo, keys to Ko (NULL: not written),
+ * both rounded once from float32 or better; Qo may be Q and Ko may be K.  With a cache, each
+ * token's keys, before any rounding, and values go to slot slots(token) (int64; slots of one
+ * call must differ; a slot outside the cache, -1 for example, is skipped).  Keys are worked out
+ * in float64 up to their codes, which so do not depend on the order of a sum.  A position
+ * outside the tables makes that token's queries and keys NaN.
+ * Argument numbers: tokens=1 q_heads=2 kv_heads=3 head_dim=4 type=5 Q=6 ldq=7 K=8 ldk=9 V=10
+ * ldv=11 q_weight=12 k_weight=13 eps=14 (finite, not negative) cosine=15 sine=16
+ * table_rows=17 rot_dim=18 style=19 positions=20 Qo=21 ldqo=22 Ko=23 ldko=24 cache=25
+ * cache_bytes=26 pages=27 page_tokens=28 slots=29 stream=30.  At most 1024 heads of either kind.
+ */
+int mipgemm_qk_norm_rope(int64_t tokens, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int type,
+                         const void *Q, int64_t ldq, const void *K, int64_t ldk,
+                         const void *V, int64_t ldv,
+                         const float *q_weight, const float *k_weight, float eps,
+                         const float *cosine, const float *sine, int64_t table_rows,
+                         int64_t rot_dim, int style, const int32_t *positions,
+                         void *Qo, int64_t ldqo, void *Ko, int64_t ldko,
+                         void *cache, size_t cache_bytes, int64_t pages, int64_t page_tokens,
+                         const int64_t *slots, void *stream);
+
+/*
+ * Slots of the cache as real numbers, tokens x kv_heads x head_dim of `type`: what the
+ * attention below computes with, for programs that move, check or re-encode a cache.  K or V
+ * may be NULL.  A slot outside the cache reads as zeros.  Argument numbers: tokens=1
+ * kv_heads=2 head_dim=3 type=4 cache=5 cache_bytes=6 pages=7 page_tokens=8 slots=9 K=10 ldk=11
+ * V=12 ldv=13 stream=14.
+ */
+int mipgemm_kv4_read(int64_t tokens, int64_t kv_heads, int64_t head_dim, int type,
+                     const void *cache, size_t cache_bytes, int64_t pages, int64_t page_tokens,
+                     const int64_t *slots, void *K, int64_t ldk, void *V, int64_t ldv, void *stream);
+
+/*
+ * Attention of a batch of requests over the 4-bit cache,
+ *     O(i) = sum over t of softmax over t (scale Q(i) . k(t)) v(t),
+ * for single tokens, drafted tokens, prompts and chunks of prompts alike.  Request r has the
+ * rows q_starts(r) .. q_starts(r + 1) - 1 of Q (requests + 1 int32, not decreasing) and
+ * kv_lengths(r) tokens in the cache (int32), token t in page block_table(r, t / page_tokens)
+ * (int32, rows table_stride apart) at t % page_tokens; its queries are the last of those
+ * tokens, so row i of n sees the keys up to kv_lengths(r) - n + i.  A row that sees no key
+ * gives zeros.  q_heads is a multiple of kv_heads; query head h reads key head
+ * h / (q_heads / kv_heads).  type is that of Q and O: MIPGEMM_BF16 or MIPGEMM_F16; rows of Q and O hold
+ * all heads, ldq and ldo elements apart, and O must not overlap Q.  scale is positive.
+ * Scores, softmax and sums are float32; p is rounded to float16 for the product with
+ * the values.
+ *
+ * The three integer arrays are read on the device alone.  q_rows (rows of Q and O), max_q
+ * and max_kv are the host's upper bounds: what the arrays say beyond them is cut to them, and
+ * keys whose page the table does not name (beyond table_stride, or a number outside 0 .. pages - 1)
+ * are not seen.  So a call with bounds that stay the same can be captured in a graph and
+ * replayed over growing lengths.  Rows of O that belong to no request are not written.
+ *
+ * `workspace` is optional: with mipgemm_attention_kv4_workspace_size bytes (16 bytes more
+ * serve where it is not 16-byte aligned), or those for q_rows rows where they are fewer, calls with few
+ * rows cut the keys into ranges that run at the same time and are joined; without, one workgroup goes
+ * through all keys of its rows.  The two differ in rounding alone.
+ * Argument numbers: requests=1 q_heads=2 kv_heads=3 head_dim=4 type=5 Q=6 ldq=7 q_rows=8
+ * q_starts=9 max_q=10 kv_lengths=11 max_kv=12 cache=13 cache_bytes=14 pages=15 page_tokens=16
+ * block_table=17 table_stride=18 scale=19 O=20 ldo=21 workspace=22 workspace_bytes=23 stream=24.
+ */
+size_t mipgemm_attention_kv4_workspace_size(int64_t requests, int64_t q_heads, int64_t kv_heads,
+                                            int64_t head_dim, int64_t max_q, int64_t max_kv);
+int mipgemm_attention_kv4(int64_t requests, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int type,
+                          const void *Q, int64_t ldq, int64_t q_rows, const int32_t *q_starts,
+                          int64_t max_q, const int32_t *kv_lengths, int64_t max_kv,
+                          const void *cache, size_t cache_bytes, int64_t pages, int64_t page_tokens,
+                          const int32_t *block_table, int64_t table_stride, float scale,
+                          void *O, int64_t ldo,
+                          void *workspace, size_t workspace_bytes, void *stream);
+
 /*
  * Static, human-readable text for a return value of the functions above.  For a
  * negative code the text gives the argument number and, in parentheses, the name

@@ -17,6 +17,10 @@ import threading
 
 ROW_MAJOR, COL_MAJOR = 0, 1
 OVERWRITE, ACCUMULATE = 0, 1
+# types of real numbers, activations of a linear layer, pairs of rotated channels
+F32, BF16, F16 = 0, 1, 2
+NONE, RELU, GELU, GELU_TANH, SILU = 0, 1, 2, 3, 4
+ROTATE_HALVES, ROTATE_PAIRS = 0, 1
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libmipgemm.so")
@@ -56,7 +60,9 @@ def exported_symbols():
             "mipgemm_packed_weights_bytes", "mipgemm_pack_weights", "mipgemm_s8s8s32_packed",
             "mipgemm_u8s8s32_packed", "mipgemm_conv_filter_sums",
             "mipgemm_conv_s8u8s32_with_sums", "mipgemm_conv_s8u8f32_with_sums", "mipgemm_conv_s8u8s8",
-            "mipgemm_s16s16s32", "mipgemm_workspace_size_s16"]
+            "mipgemm_s16s16s32", "mipgemm_workspace_size_s16",
+            "mipgemm_quantize_rows", "mipgemm_s8s8_linear", "mipgemm_kv4_bytes", "mipgemm_qk_norm_rope",
+            "mipgemm_kv4_read", "mipgemm_attention_kv4", "mipgemm_attention_kv4_workspace_size"]
 
 
 def load_library() -> ctypes.CDLL:
@@ -154,6 +160,14 @@ def load_library() -> ctypes.CDLL:
             lib.mipgemm_s8s8s32_noalloc.argtypes = _GEMM_ARGTYPES[:13] + [vp]
             lib.mipgemm_static_scratch_bytes.restype = ctypes.c_size_t
             lib.mipgemm_static_scratch_bytes.argtypes = []
+            for name in _LAYER_FORMATS:
+                fn = getattr(lib, name)
+                fn.restype = ctypes.c_int
+                fn.argtypes = [_CTYPES[f] for f in _LAYER_FORMATS[name]]
+            for name, count in (("mipgemm_kv4_bytes", 4), ("mipgemm_attention_kv4_workspace_size", 6)):
+                fn = getattr(lib, name)
+                fn.restype = ctypes.c_size_t
+                fn.argtypes = [i64] * count
             _register_native(lib)
             _lib = lib
     return _lib
@@ -168,7 +182,15 @@ _native = None  # the module, once the library is loaded
 
 _GEMM_FORMAT, _CONV_FORMAT = "qqqpqipqipqiipzs", "qqqqqqqqqpppipzs"
 _BATCHED_FORMAT, _PACKED_FORMAT = "qqqpqiqpqiqpqiqqipzs", "qqqpqippqiipzs"
+_LAYER_FORMATS = {
+    "mipgemm_quantize_rows": "qqpqipfpqps", "mipgemm_s8s8_linear": "qqqpqppqippipqpqipzs",
+    "mipgemm_qk_norm_rope": "qqqqipqpqpqppfppqqippqpqpzqqps", "mipgemm_kv4_read": "qqqipzqqppqpqs",
+    "mipgemm_attention_kv4": "qqqqipqqpqpqpzqqpqfpqpzs",
+}
+_CTYPES = {"q": ctypes.c_int64, "i": ctypes.c_int, "p": ctypes.c_void_p, "z": ctypes.c_size_t, "s": ctypes.c_void_p,
+           "f": ctypes.c_float}
 _FORMATS = {
+    **_LAYER_FORMATS,
     **{"mipgemm_" + t: _GEMM_FORMAT for t in ("s8s8s32", "u8s8s32", "s8u8s32", "s16s16s32")},
     **{"mipgemm_" + t: _GEMM_FORMAT + "f" for t in ("s8s8f32", "u8s8f32", "s8u8f32", "s8s8s8", "u8s8s8", "s8u8s8")},
     **{"mipgemm_%s_batched" % t: _BATCHED_FORMAT for t in ("s8s8s32", "u8s8s32", "s8u8s32")},
@@ -552,6 +574,54 @@ def mipgemm_s8s8s32_clocked(m, n, k, A, lda, orderA, B, ldb, orderB, C, ldc, ord
     if check and rc != 0:
         raise MipGemmError(rc, mipgemm_strerror(rc))
     return rc
+
+
+# ---- the operators between the products of a layer ----
+
+def mipgemm_quantize_rows(rows, cols, X, ldx, x_type, norm_weight, eps, Q, ldq, scales, stream=None, check=True):
+    """Q (int8), scales (float32, one per row): rows of real numbers in 8 bits, through an RMS norm where
+    ``norm_weight`` is given."""
+    return _run(check, "mipgemm_quantize_rows", rows, cols, X, ldx, x_type, norm_weight, eps, Q, ldq, scales, stream)
+
+
+def mipgemm_s8s8_linear(m, n, k, A, lda, a_scales, B, ldb, orderB, b_scales, bias, activation, R, ldr, C, ldc, c_type,
+                        workspace=None, workspace_bytes=0, stream=None, check=True):
+    """C = act(a_scales * (A * B) * b_scales + bias) + R: a linear layer on int8 operands, real numbers out."""
+    return _run(check, "mipgemm_s8s8_linear", m, n, k, A, lda, a_scales, B, ldb, orderB, b_scales, bias, activation, R, ldr,
+                C, ldc, c_type, workspace, workspace_bytes, stream)
+
+
+def mipgemm_kv4_bytes(pages, page_tokens, kv_heads, head_dim) -> int:
+    return int(load_library().mipgemm_kv4_bytes(pages, page_tokens, kv_heads, head_dim))
+
+
+def mipgemm_qk_norm_rope(tokens, q_heads, kv_heads, head_dim, type, Q, ldq, K, ldk, V, ldv, q_weight, k_weight, eps,
+                         cosine, sine, table_rows, rot_dim, style, positions, Qo, ldqo, Ko, ldko,
+                         cache=None, cache_bytes=0, pages=0, page_tokens=16, slots=None, stream=None, check=True):
+    """Heads of queries and keys normed and rotated, keys and values into the 4-bit cache (see include/mipgemm.h)."""
+    return _run(check, "mipgemm_qk_norm_rope", tokens, q_heads, kv_heads, head_dim, type, Q, ldq, K, ldk, V, ldv, q_weight,
+                k_weight, eps, cosine, sine, table_rows, rot_dim, style, positions, Qo, ldqo, Ko, ldko, cache, cache_bytes,
+                pages, page_tokens, slots, stream)
+
+
+def mipgemm_kv4_read(tokens, kv_heads, head_dim, type, cache, cache_bytes, pages, page_tokens, slots, K, ldk, V, ldv,
+                     stream=None, check=True):
+    """Slots of the 4-bit cache as real numbers."""
+    return _run(check, "mipgemm_kv4_read", tokens, kv_heads, head_dim, type, cache, cache_bytes, pages, page_tokens, slots,
+                K, ldk, V, ldv, stream)
+
+
+def mipgemm_attention_kv4_workspace_size(requests, q_heads, kv_heads, head_dim, max_q, max_kv) -> int:
+    return int(load_library().mipgemm_attention_kv4_workspace_size(requests, q_heads, kv_heads, head_dim, max_q, max_kv))
+
+
+def mipgemm_attention_kv4(requests, q_heads, kv_heads, head_dim, type, Q, ldq, q_rows, q_starts, max_q, kv_lengths, max_kv,
+                          cache, cache_bytes, pages, page_tokens, block_table, table_stride, scale, O, ldo,
+                          workspace=None, workspace_bytes=0, stream=None, check=True):
+    """O = softmax(scale * Q . keys) values over the 4-bit cache, queries the last tokens of their requests."""
+    return _run(check, "mipgemm_attention_kv4", requests, q_heads, kv_heads, head_dim, type, Q, ldq, q_rows, q_starts, max_q,
+                kv_lengths, max_kv, cache, cache_bytes, pages, page_tokens, block_table, table_stride, scale, O, ldo,
+                workspace, workspace_bytes, stream)
 
 
 ERR_STATIC_SCRATCH = -100

@@ -52,7 +52,8 @@ int run_gemm(int a_unsigned, int b_unsigned, int out_float, float scale, int64_t
              int64_t k, const void *A, int64_t lda, int orderA, const void *B, int64_t ldb,
              int orderB, void *C, int64_t ldc, int orderC, int mode, void *workspace,
              size_t workspace_bytes, void *stream, const Batch &batch = Batch(),
-             const int32_t *ksum = nullptr);  // ksum: see Problem::ksum (pre-packed weights)
+             const int32_t *ksum = nullptr,   // see Problem::ksum (pre-packed weights)
+             const LinearArgs *linear = nullptr);  // with out_float 3
 
 }  // namespace mip
 

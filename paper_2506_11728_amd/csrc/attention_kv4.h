@@ -1,0 +1,268 @@
+// Attention over the 4-bit cache (kv4.h): what its kernels share.
+//
+//     o(i) = sum over t of p(i, t) v(t) / sum over t of p(i, t),   p(i, t) = exp(scale q(i) . k(t) - max)
+// in one pass over the keys, with the running maximum and sum of the softmax in float32.  The queries of
+// all heads that share a key head are the rows of one product: row = query * shared + head.
+//
+// The products are v_mfma_f32_16x16x32_f16 on the cache's own numbers: a code's nibble under the exponent of
+// 1024 or of 64 is the float16 1024 + n (64 + n), the zero point is subtracted and the step multiplied in float16,
+// and both are exact.  Queries in bfloat16 are multiplied by a power of two that brings the row's largest
+// below 32768 and are exact as float16 wherever they are not 2^-24 times smaller than that; the power is
+// taken back in the scale of the scores.  What is rounded is p: to float16, eleven bits, less than the output's
+// own rounding.  Its sum is of the unrounded p.
+//
+// Operand layout of the instruction: lane l gives row (column) l % 16, eight k from 8 (l / 16) on; the result has
+// column l % 16 and rows 4 (l / 16) .. + 3.  Any order of k will do that both operands share.
+//   scores, transposed (tokens x rows):  lane l takes token l % 16 of a tile of sixteen and d / 4 channels in a row,
+//     which are 16 bytes of its codes (8 at d = 64) and belong to one group, so one step and zero point.
+//   output (rows x channels): the scores' result is the operand already (row l % 16, tokens 4 (l / 16) .. + 3 of two
+//     tiles), and lane l takes for it, from the same eight tokens, the channels of its word l % 16, one of
+//     the word's eight nibbles to an instruction.
+#pragma once
+#include "kv4.h"
+#include "layer_internal.h"
+
+namespace mip {
+
+typedef int v2i __attribute__((ext_vector_type(2)));
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+
+template <int D>
+struct Kv4Shape {
+  static constexpr int UNITS = D / 128 > 0 ? D / 128 : 1;   // of 128 channels
+  static constexpr int WORDS = D >= 128 ? 4 : 2;            // a lane's words of a key, per unit
+  static constexpr int NIBBLES = D >= 128 ? 8 : 4;          // a lane's channels of a value, per unit
+  static constexpr int KEY_STEPS = UNITS * WORDS;           // instructions for the scores of a tile
+  static constexpr int CHANNELS = UNITS * NIBBLES;          // instructions for the output of two tiles
+  // channel of a query that meets nibble e of word w, unit u of lane group h
+  __host__ __device__ static constexpr int key_channel(int u, int w, int h, int e) {
+    return D >= 128 ? 128 * u + 32 * h + 8 * w + e : 16 * h + 8 * w + e;
+  }
+  // channel that instruction (u, j) gives column c of the output
+  __host__ __device__ static constexpr int value_channel(int u, int j, int c) {
+    return D >= 128 ? 128 * u + 8 * c + j : 4 * c + j;
+  }
+};
+
+// Codes of a tile's keys and of the values of four of its tokens, and their pairs, as they come from memory.
+template <int D>
+struct Kv4Tile {
+  using S = Kv4Shape<D>;
+  uint32_t key[S::UNITS][S::WORDS];
+  uint32_t key_pair[S::UNITS];
+  v4u value[S::UNITS];
+  v2i value_pair[S::UNITS];
+};
+
+// part: the head's part of the tile's page; first: the tile's first token in the page.  A lane's offsets
+// in a part that do not depend on the tile are worked out once.
+template <int D>
+struct Kv4Reader {
+  using S = Kv4Shape<D>;
+  int key, key_pair[S::UNITS], value, value_pair[S::UNITS];  // bytes
+  __device__ __forceinline__ Kv4Reader(int log_page, int lane) {
+    const int c = lane & 15, h = lane >> 4, page = 1 << log_page;
+    const Kv4Layout L(page, D);
+    key = c * (D / 2) + h * (4 * S::WORDS);
+    value = (int)L.values + 16 * (h * (D / 8) + (D >= 128 ? c : c >> 1));
+#pragma unroll
+    for (int u = 0; u < S::UNITS; ++u) {
+      key_pair[u] = (int)L.key_pairs + 2 * (((D >= 128 ? 4 * u + h : h >> 1) << log_page) + c);
+      value_pair[u] = (int)L.value_pairs + 2 * (((D >= 128 ? 4 * u + (c >> 2) : c >> 3) << log_page) + 4 * h);
+    }
+  }
+  // COUNT words of a key from instruction `from` on (all of them of one unit), and its group's pair
+  template <int COUNT>
+  __device__ __forceinline__ void load_keys(const uint8_t *part, int first, int from, uint32_t (&w)[COUNT], uint32_t &pair) const {
+    static_assert(COUNT == 1 || COUNT == 2 || COUNT == 4, "whole loads");
+    const int u = from / S::WORDS;
+    const uint8_t *k = part + first * (D / 2) + key + 64 * u + 4 * (from % S::WORDS);
+    if constexpr (COUNT == 4) {
+      const v4u x = *reinterpret_cast<const v4u *>(k);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = x[i];
+    } else if constexpr (COUNT == 2) {
+      const v2i x = *reinterpret_cast<const v2i *>(k);
+      w[0] = x[0];
+      w[1] = x[1];
+    } else {
+      w[0] = *reinterpret_cast<const uint32_t *>(k);
+    }
+    pair = *reinterpret_cast<const uint16_t *>(part + 2 * first + (u ? key_pair[S::UNITS - 1] : key_pair[0]));
+  }
+  __device__ __forceinline__ void load_values(const uint8_t *part, int first, v4u (&w)[S::UNITS], v2i (&pair)[S::UNITS]) const {
+    const uint8_t *v = part + first * (D / 2) + value;
+#pragma unroll
+    for (int u = 0; u < S::UNITS; ++u) {
+      w[u] = *reinterpret_cast<const v4u *>(v + 256 * u);
+      pair[u] = *reinterpret_cast<const v2i *>(part + 2 * first + value_pair[u]);
+    }
+  }
+  __device__ __forceinline__ void load(const uint8_t *part, int first, Kv4Tile<D> &t) const {
+#pragma unroll
+    for (int u = 0; u < S::UNITS; ++u) load_keys<S::WORDS>(part, first, u * S::WORDS, t.key[u], t.key_pair[u]);
+    load_values(part, first, t.value, t.value_pair);
+  }
+};
+
+__device__ __forceinline__ v2h as_halves(uint32_t w) { return __builtin_bit_cast(v2h, w); }
+
+// Steps and negated zero points of two pairs (one in either half of `pairs`).
+struct Kv4Scale {
+  v2h s, z1024, z64;  // s, -(1024 + z), -(64 + z)
+  __device__ __forceinline__ explicit Kv4Scale(uint32_t pairs) {
+    s = as_halves((pairs & 0x00ff00ffu) << 7);
+    // z + 128 under the exponent of -1024, less the 128
+    z1024 = as_halves(((pairs >> 8) & 0x00ff00ffu) ^ 0xe480e480u) + (_Float16)128.0f;
+    z64 = z1024 + (_Float16)960.0f;
+  }
+  // nibbles at bits 0 and 16, and at bits 4 and 20
+  __device__ __forceinline__ v2h low(uint32_t w) const { return (as_halves((w & 0x000f000fu) | 0x64006400u) + z1024) * s; }
+  __device__ __forceinline__ v2h high(uint32_t w) const { return (as_halves((w & 0x00f000f0u) | 0x54005400u) + z64) * s; }
+};
+
+__device__ __forceinline__ v8h join(v2h a, v2h b, v2h c, v2h d) {
+  return v8h{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// Operand of the scores from word w of a lane's keys: channels in the order 0 4 1 5 2 6 3 7.
+__device__ __forceinline__ v8h key_operand(uint32_t w, const Kv4Scale &g) {
+  const uint32_t x = w >> 8;
+  return join(g.low(w), g.high(w), g.low(x), g.high(x));
+}
+
+// Operands of the output from the values of two tiles: instruction j of unit u, tokens in the order of the
+// score's result.
+template <int D>
+struct Kv4Values {
+  using S = Kv4Shape<D>;
+  Kv4Scale g[4];
+  uint32_t selector;  // bytes of the first pair of channels (d = 64: a lane takes half a word)
+  const v4u a, b;
+  __device__ __forceinline__ Kv4Values(v4u a, v4u b, v2i pa, v2i pb, int lane)
+      : g{Kv4Scale(pa[0]), Kv4Scale(pa[1]), Kv4Scale(pb[0]), Kv4Scale(pb[1])},
+        selector(0x0c040c00u + (D >= 128 ? 0u : (lane & 1) * 0x00020002u)), a(a), b(b) {}
+  // channels 2 k and 2 k + 1 of the lane
+  __device__ __forceinline__ void pair(int k, v8h &even, v8h &odd) const {
+    const uint32_t sel = selector + k * 0x00010001u;
+    const uint32_t x0 = __builtin_amdgcn_perm(a[1], a[0], sel), x1 = __builtin_amdgcn_perm(a[3], a[2], sel);
+    const uint32_t x2 = __builtin_amdgcn_perm(b[1], b[0], sel), x3 = __builtin_amdgcn_perm(b[3], b[2], sel);
+    even = join(g[0].low(x0), g[1].low(x1), g[2].low(x2), g[3].low(x3));
+    odd = join(g[0].high(x0), g[1].high(x1), g[2].high(x2), g[3].high(x3));
+  }
+};
+
+__device__ __forceinline__ v4f multiply(v8h a, v8h b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+// A request as the kernels see it: its rows of queries, its keys.  The device's numbers are cut to what the
+// host was told, so that no value of theirs reads or writes outside the buffers.
+struct Request {
+  int64_t q0;       // first row of Q
+  int queries, keys;
+};
+__device__ __forceinline__ Request request_of(const AttentionArgs &P, int r) {
+  int64_t a = P.q_starts[r], b = P.q_starts[r + 1];
+  a = a < 0 ? 0 : (a > P.q_rows ? P.q_rows : a);
+  b = b < a ? a : (b > P.q_rows ? P.q_rows : b);
+  int64_t queries = b - a, keys = P.kv_lengths[r];
+  queries = queries > P.max_q ? P.max_q : queries;
+  keys = keys < 0 ? 0 : (keys > P.max_kv ? P.max_kv : keys);
+  return {a, (int)queries, (int)keys};
+}
+// The head's part of the page of a token, or null where the table names no page there.
+__device__ __forceinline__ const uint8_t *part_of(const AttentionArgs &P, int r, int head, int64_t token, int64_t block) {
+  const int64_t at = token >> P.log_page;
+  const int page = at < P.table_stride ? P.block_table[r * P.table_stride + at] : -1;
+  return page >= 0 && page < P.pages ? P.cache + ((int64_t)page * P.kv_heads + head) * block : nullptr;
+}
+
+constexpr float LOWEST = -3.402823466e38f;
+// p is 2^(score - base) in float16, base the row's maximum less HEAD when it was last set: up to 2^LIMIT before
+// the sums have to be rescaled, and not lost before it is 2^-31 of the largest.
+constexpr float HEAD = 7.0f, LIMIT = 15.0f;
+
+// Queries of a row as operands of the scores, and what a score is multiplied by to be a power of two's exponent.
+// at: the row's first channel in Q; here: whether the row exists (else zeros).
+template <int D, int TYPE>
+__device__ __forceinline__ float load_queries(const AttentionArgs &P, int64_t at, bool here, int h, v8h (&q)[Kv4Shape<D>::KEY_STEPS]) {
+  using S = Kv4Shape<D>;
+  constexpr int ORDER[8] = {0, 4, 1, 5, 2, 6, 3, 7};
+  v4f x[S::KEY_STEPS][2];
+  float top = 0.0f;
+#pragma unroll
+  for (int i = 0; i < S::KEY_STEPS; ++i)
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      x[i][half] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+      if (here) x[i][half] = load_real4(P.Q, at + S::key_channel(i / S::WORDS, i % S::WORDS, h, 4 * half), TYPE);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(x[i][half][e]));
+    }
+  float by = 1.0f, back = 1.0f;
+  if (TYPE == REAL_BF16) {
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    int e = (__float_as_int(top) >> 23) - 127;  // top < 2^(e + 1)
+    e = e < -100 ? -100 : e;
+    by = __int_as_float((127 + 14 - e) << 23);
+    back = __int_as_float((127 - 14 + e > 0 ? 127 - 14 + e : 1) << 23);
+  }
+#pragma unroll
+  for (int i = 0; i < S::KEY_STEPS; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) q[i][e] = (_Float16)(x[i][ORDER[e] / 4][ORDER[e] % 4] * by);
+  // (never zero, which would make a NaN of a masked score)
+  return fmaxf(P.scale * 1.4426950408889634f * back, 1.2e-38f);
+}
+
+// p of 32 keys for a wave's sixteen rows (lane: row l % 16, tokens 4 (l / 16) .. + 3 of two tiles) from their scores,
+// as the operand of the output.  Only where a score has risen past LIMIT do the lanes of a row have to agree on a
+// new base (top), and are its sums rescaled.
+template <int CHANNELS>
+__device__ __forceinline__ v8h weights(const v4f (&score)[2], float scale, float &top, float &total, v4f (&out)[CHANNELS], int h) {
+  float x[8];
+  // A fused multiply-add keeps what the product's rounding would lose, but against a base that is a rounded product
+  // itself the difference of two large numbers is no longer zero where they are equal: past 2^20 both are rounded.
+  auto exponents = [&] {
+    if (__any(fabsf(top) > 1048576.0f)) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = __fsub_rn(__fmul_rn(score[e / 4][e % 4], scale), top);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = __builtin_fmaf(score[e / 4][e % 4], scale, -top);
+    }
+  };
+  exponents();
+  float largest = LOWEST;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) largest = fmaxf(largest, x[e]);
+  if (__any(largest > LIMIT)) {
+    largest = LOWEST;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) largest = fmaxf(largest, __fmul_rn(score[e / 4][e % 4], scale));
+    largest = fmaxf(largest, __shfl_xor(largest, 16));
+    largest = fmaxf(largest, __shfl_xor(largest, 32));
+    const float moved = largest - HEAD > top ? largest - HEAD : top;
+    const float less = __builtin_amdgcn_exp2f(top - moved);
+    top = moved;
+    total *= less;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float by = __shfl(less, 4 * h + e);
+#pragma unroll
+      for (int j = 0; j < CHANNELS; ++j) out[j][e] *= by;
+    }
+    exponents();
+  }
+  v8h p;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float y = __builtin_amdgcn_exp2f(x[e]);
+    total += y;
+    p[e] = (_Float16)y;
+  }
+  return p;
+}
+
+}  // namespace mip

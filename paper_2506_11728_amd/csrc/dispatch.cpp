@@ -534,8 +534,8 @@ static Plan fastest_tiles(const Problem &p, Plan plan) {
 Plan choose_plan(const Problem &p) {
   const int64_t kComputeUnits = compute_units();
   if (p.m == 0 || p.n == 0) return {KIND_NONE, SHAPE_64, 1};
-  // (the zero fill writes words; an int8 output of an empty sum goes through the simple kernel)
-  if (p.k == 0) return {p.accumulate ? KIND_NONE : (p.out_float == 2 ? KIND_SIMPLE : KIND_FILL), SHAPE_64, 1};
+  // (the zero fill writes words; an int8 output of an empty sum, and a linear layer's, go through the simple kernel)
+  if (p.k == 0) return {p.accumulate ? KIND_NONE : (p.out_float >= 2 ? KIND_SIMPLE : KIND_FILL), SHAPE_64, 1};
   Plan plan;
   if (!forced_plan(p, &plan)) {
     // The largest tile that still gives most compute units a workgroup; a

@@ -12,6 +12,7 @@
 // multiplied, the write-back stops at the edge of C.
 #include "dma_common.h"
 #include "epilogue16.h"
+#include "linear.h"
 #include "tuning.h"
 
 namespace mip {
@@ -44,6 +45,9 @@ struct DmaParams {
   // the values to add to beforehand).
   int per_range, longer;  // blocks of a range; the first `longer` have one more
   int atomic;
+};
+struct DmaLinearK128Params : DmaParams {
+  LinearArgs linear;
 };
 
 // ---------------------------------------------------------------------------
@@ -173,7 +177,8 @@ struct Stage16 {
 // UNS: 0 both operands signed, 1 A unsigned, 2 B unsigned; 3 and 4: as 1 and 2 with the k sums
 // of the signed operand read from P.ksum (pre-packed weights carry them) instead of being
 // accumulated from the fragments in the loop, which costs four dot-product instructions per
-// fragment of the signed operand between the matrix instructions.
+// fragment of the signed operand between the matrix instructions.  LINEAR_OUT: both signed, the
+// write-back of a linear layer.
 //
 // GENERAL (with RAGGED): m and n need not be whole tiles and the operands need no padding
 // (loads that would leave an operand are redirected inside it); a strided operand's extent
@@ -181,7 +186,8 @@ struct Stage16 {
 // sums meet in C through atomics: the form for problems with too few tiles to occupy the
 // device and a long k.
 template <int BM, int BN, bool A_KC, bool B_KC, int UNS, bool RAGGED = false, bool GENERAL = false>
-__global__ __launch_bounds__(NTHREADS) void dma128_kernel(DmaParams P) {
+__global__ __launch_bounds__(NTHREADS) void dma128_kernel(std::conditional_t<UNS == LINEAR_OUT, DmaLinearK128Params, DmaParams> P) {
+  constexpr bool FIX = UNS != 0 && UNS != LINEAR_OUT;  // one operand unsigned
   constexpr bool FLIP_A = UNS == 1 || UNS == 3, FLIP_B = UNS == 2 || UNS == 4;
   constexpr bool SUM_A = UNS == 2, SUM_B = UNS == 1;
   using TS = Tile16<BM, BN>;
@@ -320,7 +326,7 @@ __global__ __launch_bounds__(NTHREADS) void dma128_kernel(DmaParams P) {
   publish_barrier<0>();
 #pragma unroll
   for (int r = 0; r < NREADS; ++r) read_frag(0, 0, 0, r, fa[0], fb[0]);
-  if (UNS != 0) {
+  if (FIX) {
 #pragma unroll
     for (int r = 0; r < NREADS; ++r) fix_frag(r, fa[0], fb[0]);
     __builtin_amdgcn_sched_barrier(0);
@@ -364,7 +370,7 @@ __global__ __launch_bounds__(NTHREADS) void dma128_kernel(DmaParams P) {
       if (s >= READ_FROM && (s - READ_FROM) % READ_EVERY == 0) {
         const int r = (s - READ_FROM) / READ_EVERY;
         if (r < NREADS) reader(r);
-        if (UNS != 0 && r >= FIX_LAG && r - FIX_LAG < NREADS) fixer(r - FIX_LAG);
+        if (FIX && r >= FIX_LAG && r - FIX_LAG < NREADS) fixer(r - FIX_LAG);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -417,6 +423,13 @@ __global__ __launch_bounds__(NTHREADS) void dma128_kernel(DmaParams P) {
       sumA, sumB, FLIP_A, FLIP_B, lane,
       reinterpret_cast<int32_t *>(smem) + 4 * Patch16<FN>::WORDS + wave * Correction16<FM, FN>::WORDS);
   const int64_t mw = m0 + wm * WM, nw = n0 + wn * WN;  // the wave's sub-tile
+  if constexpr (UNS == LINEAR_OUT) {
+    if (!RAGGED || (mw + WM <= P.m && nw + WN <= P.n))
+      store_linear16<FM, FN, true>(acc, P.linear, mw, nw, WM, WN, lane, patch);
+    else if (mw < P.m && nw < P.n)
+      store_linear16<FM, FN, false>(acc, P.linear, mw, nw, P.m - mw, P.n - nw, lane, patch);
+    return;
+  }
   // an int8 output is a matrix of bytes, ldc counted in bytes
   void *C = P.out_float == 2 ? static_cast<void *>(reinterpret_cast<int8_t *>(P.C) + mw * P.ldc + nw)
                              : static_cast<void *>(P.C + mw * P.ldc + nw);
@@ -424,16 +437,16 @@ __global__ __launch_bounds__(NTHREADS) void dma128_kernel(DmaParams P) {
   if constexpr (GENERAL && BM == 128 && BN == 128) {  // (k ranges exist on the small tile only)
     if (P.atomic) {
       if (mw < P.m && nw < P.n)
-        add_blocks16_atomic<FM, FN, UNS != 0>(acc, P.C + mw * P.ldc + nw, P.ldc, P.m - mw, P.n - nw, lane, patch, corr);
+        add_blocks16_atomic<FM, FN, FIX>(acc, P.C + mw * P.ldc + nw, P.ldc, P.m - mw, P.n - nw, lane, patch, corr);
       added = true;
     }
   }
   if (added) {
   } else if (!RAGGED || (mw + WM <= P.m && nw + WN <= P.n))
-    store_blocks16<FM, FN, true, UNS != 0>(acc, C, P.ldc, WM, WN, P.accumulate != 0, P.out_float, lane, patch,
+    store_blocks16<FM, FN, true, FIX>(acc, C, P.ldc, WM, WN, P.accumulate != 0, P.out_float, lane, patch,
                                            P.scale, corr);
   else if (mw < P.m && nw < P.n)
-    store_blocks16<FM, FN, false, UNS != 0>(acc, C, P.ldc, P.m - mw, P.n - nw, P.accumulate != 0, P.out_float,
+    store_blocks16<FM, FN, false, FIX>(acc, C, P.ldc, P.m - mw, P.n - nw, P.accumulate != 0, P.out_float,
                                             lane, patch, P.scale, corr);
 }
 

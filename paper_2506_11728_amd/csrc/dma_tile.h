@@ -25,6 +25,7 @@
 // tensor; a tap that falls outside the image reads a block of zeros instead.
 #pragma once
 #include "dma_common.h"
+#include "linear.h"
 
 namespace mip {
 
@@ -54,6 +55,9 @@ struct DmaTileParams {
   const int32_t *ksum;    // UNS 3 and 4: the k sums of the signed operand (see Problem::ksum)
   int64_t a_sb, b_sb, c_sb;  // byte / element offsets of problem z of a batch (blockIdx.z)
 };
+struct DmaLinearParams : DmaTileParams {
+  LinearArgs linear;
+};
 struct DmaConvParams : DmaTileParams {
   ConvGeom conv;
   Divisor per_image, per_row;  // by the output positions of an image and of a row of one
@@ -61,9 +65,10 @@ struct DmaConvParams : DmaTileParams {
 
 // UNS: 0 both operands signed, 1 A unsigned, 2 B unsigned; 3 and 4: as 1 and 2 with the k sums
 // of the signed operand read from P.ksum instead of being accumulated from the fragments
-// (with split k by the first range alone).
+// (with split k by the first range alone).  LINEAR_OUT: both signed, the write-back of a linear layer.
 template <int BM, int BN, bool A_KC, bool B_KC, int UNS, bool CONV = false, int GROUPS = 1>
-__global__ __launch_bounds__(NTHREADS *GROUPS) void dma_tile_kernel(std::conditional_t<CONV, DmaConvParams, DmaTileParams> P) {
+__global__ __launch_bounds__(NTHREADS *GROUPS) void dma_tile_kernel(
+    std::conditional_t<CONV, DmaConvParams, std::conditional_t<UNS == LINEAR_OUT, DmaLinearParams, DmaTileParams>> P) {
   constexpr bool FLIP_A = UNS == 1 || UNS == 3, FLIP_B = UNS == 2 || UNS == 4;
   constexpr bool SUM_A = UNS == 2, SUM_B = UNS == 1;
   static_assert(!CONV || (A_KC && B_KC), "the lowered matrix and the filters are k-contiguous");
@@ -366,6 +371,14 @@ __global__ __launch_bounds__(NTHREADS *GROUPS) void dma_tile_kernel(std::conditi
     }
   }
   const int64_t mw = m0 + wm * (BM / 2), nw = n0 + wn * (BN / 2);  // the wave's sub-tile
+  if constexpr (UNS == LINEAR_OUT) {
+    int32_t *patch = reinterpret_cast<int32_t *>(patches + wave * STORE_PATCH_BYTES);
+    if (m0 + BM <= P.m && n0 + BN <= P.n)
+      store_linear32<FM, FN, true>(acc, P.linear, mw, nw, P.m - mw, P.n - nw, lane, patch);
+    else if (mw < P.m && nw < P.n)
+      store_linear32<FM, FN, false>(acc, P.linear, mw, nw, P.m - mw, P.n - nw, lane, patch);
+    return;
+  }
   if (mw < P.m && nw < P.n) {
     if (P.out_float == 2) {  // int8 output: C is a matrix of bytes
       int8_t *Q = reinterpret_cast<int8_t *>(P.C) + mw * P.ldc + nw;
@@ -532,8 +545,18 @@ hipError_t launch_dma_tile_for(const Problem &p, int splits, hipStream_t s) {
         filter_sums ? dma_tile_kernel<BM, BN, true, true, 3, true, GROUPS> : dma_tile_kernel<BM, BN, true, true, 1, true, GROUPS>;
     kernel = reinterpret_cast<const void *>(gather);
   }
+  DmaLinearParams PL;
+  const void *args = &P;
+  if (p.linear) {  // (A row-major, both operands signed: checked where Problem::linear is set)
+    static_cast<DmaTileParams &>(PL) = P;
+    PL.linear = *p.linear;
+    args = &PL;
+    void (*linear)(DmaLinearParams) = b_kc ? dma_tile_kernel<BM, BN, true, true, LINEAR_OUT, false, GROUPS>
+                                           : dma_tile_kernel<BM, BN, true, false, LINEAR_OUT, false, GROUPS>;
+    kernel = reinterpret_cast<const void *>(linear);
+  }
   const hipError_t e = allow_dynamic_lds(kernel, lds);
-  return e != hipSuccess ? e : launch_with(kernel, grid, NTHREADS * GROUPS, lds, s, &P);
+  return e != hipSuccess ? e : launch_with(kernel, grid, NTHREADS * GROUPS, lds, s, args);
 }
 
 }  // namespace mip

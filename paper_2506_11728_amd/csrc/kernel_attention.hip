@@ -1,0 +1,531 @@
+// Attention over the 4-bit cache: the kernel for few rows (single tokens and drafted ones), the one for many
+// (prompts and their chunks), and the one that joins ranges of keys.
+//
+// Few rows: bound by the cache's bytes.  A workgroup takes the rows of one request and key head (16 or 32 of them) and a
+// range of its keys; its four waves take steps of 32 keys in turn, each with a running maximum, sum and
+// output of its own, which meet in LDS at the end.  Where requests and heads are too few to occupy the device the
+// keys are cut into ranges, and a second, small kernel joins them.
+#include "attention_kv4.h"
+
+namespace mip {
+
+namespace {
+
+constexpr int WAVES = 4, STEP = 32;  // keys of a wave's step: two tiles
+
+// A range's result for a row in scratch memory: D sums, then maximum and sum of the softmax.
+template <int D>
+constexpr int PARTIAL = D + 4;
+
+template <int D, int TYPE, int RT>
+__global__ __launch_bounds__(64 * WAVES) void attention_rows_kernel(AttentionArgs P) {
+  using S = Kv4Shape<D>;
+  extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+  auto sums = reinterpret_cast<float (*)[16][D + 4]>(smem);  // a wave's: sixteen rows
+  __shared__ float tops[WAVES][16], totals[WAVES][16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c = lane & 15, h = lane >> 4;
+  const int range = blockIdx.x % P.ranges, of_all = P.first + blockIdx.x / P.ranges, r = blockIdx.z;
+  const int head = of_all % P.kv_heads, tile = of_all / P.kv_heads;
+  const Request req = request_of(P, r);
+  const int rows = req.queries * P.shared, row0 = tile * (16 * RT);
+  if (row0 >= rows) return;
+  const int64_t block = Kv4Layout(1 << P.log_page, D).block;
+  // keys that any row of the tile sees
+  const int last_query = (row0 + 16 * RT < rows ? row0 + 16 * RT - 1 : rows - 1) / P.shared;
+  const int seen = req.keys - req.queries + last_query + 1;
+  const int begin = range * P.span, end = P.partials ? (seen < begin + P.span ? seen : begin + P.span) : seen;
+  if (range > 0 && begin >= end) return;
+
+  v8h q[RT][S::KEY_STEPS];
+  float scale[RT], top[RT], total[RT];
+  int sees[RT];  // keys that the row sees
+  v4f out[RT][S::CHANNELS];
+  int fewest = 0x7fffffff;
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int row = row0 + 16 * t + c;
+    const bool here = row < rows;
+    const int query = here ? row / P.shared : 0;
+    const int64_t at = (req.q0 + query) * P.ldq + (int64_t)(head * P.shared + (row - query * P.shared)) * D;
+    scale[t] = load_queries<D, TYPE>(P, at, here, h, q[t]);
+    sees[t] = here ? req.keys - req.queries + query + 1 : 0;
+    const int first_query = (row0 + 16 * t) / P.shared;
+    const int least = row0 + 16 * t + 15 < rows ? req.keys - req.queries + first_query + 1 : 0;
+    fewest = least < fewest ? least : fewest;
+    top[t] = LOWEST;
+    total[t] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < S::CHANNELS; ++j) out[t][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+
+  const Kv4Reader<D> reader(P.log_page, lane);
+  const int steps = end > begin ? (end - begin + STEP - 1) / STEP : 0;
+  const int mask = (1 << P.log_page) - 1;
+  Kv4Tile<D> next[2];
+  bool named[2];  // the table names a page for the tile
+  auto fetch = [&](int step) {
+    const int token = begin + step * STEP;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int first = token + 16 * u;
+      const uint8_t *part = first < end ? part_of(P, r, head, first, block) : nullptr;
+      named[u] = part != nullptr;
+      reader.load(named[u] ? part : P.cache, named[u] ? first & mask : 0, next[u]);
+    }
+  };
+  if (wave < steps) fetch(wave);
+  for (int step = wave; step < steps; step += WAVES) {
+    Kv4Tile<D> now[2] = {next[0], next[1]};
+    const bool known[2] = {named[0], named[1]};
+    if (step + WAVES < steps) fetch(step + WAVES);
+    const int token = begin + step * STEP;
+
+    v4f score[RT][2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int t = 0; t < RT; ++t) score[t][u] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int n = 0; n < S::UNITS; ++n) {
+        const Kv4Scale g(now[u].key_pair[n] * 0x00010001u);
+#pragma unroll
+        for (int w = 0; w < S::WORDS; ++w) {
+          const v8h k = key_operand(now[u].key[n][w], g);
+#pragma unroll
+          for (int t = 0; t < RT; ++t) score[t][u] = multiply(k, q[t][n * S::WORDS + w], score[t][u]);
+        }
+      }
+    }
+    if (token + STEP > fewest || !known[0] || !known[1]) {  // wave-uniform: some row does not see all of them
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int at = token + 16 * u + 4 * h + e;
+#pragma unroll
+          for (int t = 0; t < RT; ++t)
+            if (at >= sees[t] || !known[u]) score[t][u][e] = -__builtin_inff();
+        }
+      // what lies behind the last key, and in pages that are none, is no number: a step of zero makes it zero
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int n = 0; n < S::UNITS; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (token + 16 * u + 4 * h + e >= end || !known[u])
+              now[u].value_pair[n][e / 2] &= e & 1 ? 0x0000ffff : (int)0xffff0000;
+    }
+    v8h p[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+      p[t] = weights(score[t], scale[t], top[t], total[t], out[t], h);
+#pragma unroll
+    for (int n = 0; n < S::UNITS; ++n) {
+      const Kv4Values<D> values(now[0].value[n], now[1].value[n], now[0].value_pair[n], now[1].value_pair[n], lane);
+#pragma unroll
+      for (int k = 0; k < S::NIBBLES / 2; ++k) {
+        v8h even, odd;
+        values.pair(k, even, odd);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          v4f &a = out[t][n * S::NIBBLES + 2 * k], &b = out[t][n * S::NIBBLES + 2 * k + 1];
+          a = multiply(p[t], even, a);
+          b = multiply(p[t], odd, b);
+        }
+      }
+    }
+  }
+
+  // the waves' results meet: thread 16 row + part takes D / 16 channels in a row of one row
+  const int row_in = tid >> 4, part = tid & 15;
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    float all = total[t];
+    all += __shfl_xor(all, 16);
+    all += __shfl_xor(all, 32);
+    if (t > 0) __syncthreads();
+    if (h == 0) {
+      tops[wave][c] = top[t];
+      totals[wave][c] = all;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int j = 0; j < S::CHANNELS; ++j)
+        sums[wave][4 * h + e][S::value_channel(j / S::NIBBLES, j % S::NIBBLES, c)] = out[t][j][e];
+    __syncthreads();
+    const int row = row0 + 16 * t + row_in;
+    float m = tops[0][row_in], l = 0.0f, o[D / 16];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) m = fmaxf(m, tops[w][row_in]);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) o[i] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const float by = __builtin_amdgcn_exp2f(tops[w][row_in] - m);
+      l += by * totals[w][row_in];
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) o[i] += by * sums[w][row_in][part * (D / 16) + i];
+    }
+    if (row >= rows) continue;
+    const int query = row / P.shared, within = row - query * P.shared;
+    if (P.partials) {
+      const int64_t row_of_all = ((int64_t)(req.q0 + query) * P.kv_heads + head) * P.shared + within;
+      float *to = P.partials + (row_of_all * P.ranges + range) * PARTIAL<D>;
+#pragma unroll
+      for (int i = 0; i < D / 16; i += 4)
+        *reinterpret_cast<v4f *>(to + part * (D / 16) + i) = v4f{o[i], o[i + 1], o[i + 2], o[i + 3]};
+      if (part == 0) *reinterpret_cast<v2f *>(to + D) = v2f{m, l};
+    } else {
+      const float by = l != 0.0f ? 1.0f / l : 0.0f;  // (a row that sees nothing: zeros)
+      const int64_t at = (req.q0 + query) * P.ldo + (int64_t)(head * P.shared + within) * D + part * (D / 16);
+#pragma unroll
+      for (int i = 0; i < D / 16; i += 4)
+        store_real4(P.O, at + i, TYPE, v4f{o[i], o[i + 1], o[i + 2], o[i + 3]} * by);
+    }
+  }
+}
+
+// The kernel for many rows.  A workgroup of W waves takes 16 RT W rows of one request and key head; tiles of 64 keys
+// are brought from codes to float16 once for all of them, each wave its share, and lie in LDS as the operands the
+// instructions take, 1 KB each, so that every read is sixteen bytes a lane in a row.  Two stages: the codes of the
+// tile after next are on their way while the next one's are written and the present one is multiplied.
+template <int D, int TYPE, int RT, int W>
+__global__ __launch_bounds__(64 * W, W / 4) void attention_tiles_kernel(AttentionArgs P) {
+  using S = Kv4Shape<D>;
+  constexpr int TILE = 64, KEYS = 4 * S::KEY_STEPS, VALUES = 2 * S::CHANNELS, STAGE = (KEYS + VALUES) * 1024;
+  constexpr int KEY_PARTS = W / 4, KEY_EACH = S::KEY_STEPS / KEY_PARTS;  // a wave's share of a tile of sixteen keys
+  constexpr int PAIRS = S::CHANNELS / 2, VALUE_PARTS = W / 2 < PAIRS ? W / 2 : PAIRS, VALUE_EACH = PAIRS / VALUE_PARTS;
+  extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+  __shared__ int named[2][4];  // whether the table names a page for the tiles of sixteen of a stage
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c = lane & 15, h = lane >> 4;
+  const int range = blockIdx.x % P.ranges, r = blockIdx.z;
+  // the last rows of a prompt see the most keys: they begin first
+  const int of_all = P.first + (int)(gridDim.x / P.ranges) - 1 - (int)(blockIdx.x / P.ranges);
+  const int head = of_all % P.kv_heads, row0 = of_all / P.kv_heads * (16 * RT * W);
+  const Request req = request_of(P, r);
+  const int rows = req.queries * P.shared;
+  if (row0 >= rows) return;
+  const int64_t block = Kv4Layout(1 << P.log_page, D).block;
+  const int before = req.keys - req.queries + 1;  // keys that the first query sees
+  auto sees_of = [&](int row) { return before + row / P.shared; };
+  const int seen = sees_of(row0 + 16 * RT * W < rows ? row0 + 16 * RT * W - 1 : rows - 1);
+  const int begin = range * P.span, end = P.partials && begin + P.span < seen ? begin + P.span : seen;
+  if (range > 0 && begin >= end) return;
+
+  const int wave_row = row0 + wave * (16 * RT);
+  v8h q[RT][S::KEY_STEPS];
+  float scale[RT], top[RT], total[RT];
+  int sees[RT];
+  v4f out[RT][S::CHANNELS];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int row = wave_row + 16 * t + c;
+    const bool here = row < rows;
+    const int query = here ? row / P.shared : 0;
+    const int64_t at = (req.q0 + query) * P.ldq + (int64_t)(head * P.shared + (row - query * P.shared)) * D;
+    scale[t] = load_queries<D, TYPE>(P, at, here, h, q[t]);
+    sees[t] = here ? before + query : 0;
+    top[t] = LOWEST;
+    total[t] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < S::CHANNELS; ++j) out[t][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  // the fewest and the most keys that a row of the wave sees
+  const int wave_end = wave_row + 16 * RT < rows ? wave_row + 16 * RT : rows;
+  const int fewest = wave_row + 16 * RT <= rows ? sees_of(wave_row) : 0, most = wave_row < rows ? sees_of(wave_end - 1) : 0;
+
+  const Kv4Reader<D> reader(P.log_page, lane);
+  const int mask = (1 << P.log_page) - 1;
+  const int tiles = end > begin ? (end - begin + TILE - 1) / TILE : 0;
+  // a wave's share: keys of tile `wave % 4`, values of the tiles 2 (wave % 2) and the one after
+  const int key_tile = wave & 3, key_part = wave >> 2, step = wave & 1, value_part = wave >> 1;
+  uint32_t key[KEY_EACH], key_pair;
+  v4u value[2][S::UNITS];
+  v2i value_pair[2][S::UNITS];
+  bool key_named, value_named[2];
+  int taken = 0;  // the token that the codes in registers begin with
+  auto fetch = [&](int tile) {
+    taken = begin + tile * TILE;
+    {
+      const int first = taken + 16 * key_tile;
+      const uint8_t *part = first < end ? part_of(P, r, head, first, block) : nullptr;
+      key_named = part != nullptr;
+      reader.template load_keys<KEY_EACH>(key_named ? part : P.cache, key_named ? first & mask : 0, key_part * KEY_EACH, key, key_pair);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int first = taken + 32 * step + 16 * i;
+      const uint8_t *part = first < end ? part_of(P, r, head, first, block) : nullptr;
+      value_named[i] = part != nullptr;
+      reader.load_values(value_named[i] ? part : P.cache, value_named[i] ? first & mask : 0, value[i], value_pair[i]);
+    }
+  };
+  auto unpack = [&](int stage) {
+    uint8_t *to = smem + stage * STAGE + 16 * lane;
+    const Kv4Scale g(key_pair * 0x00010001u);
+#pragma unroll
+    for (int i = 0; i < KEY_EACH; ++i)
+      *reinterpret_cast<v8h *>(to + (key_tile * S::KEY_STEPS + key_part * KEY_EACH + i) * 1024) = key_operand(key[i], g);
+    if (key_part == 0 && lane == 0) named[stage][key_tile] = key_named;
+    if (value_part >= VALUE_PARTS) return;
+    // what lies behind the last key, and in pages that are none, is no number: a step of zero makes it zero
+    if (taken + TILE > end || !value_named[0] || !value_named[1]) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int n = 0; n < S::UNITS; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (taken + 32 * step + 16 * i + 4 * h + e >= end || !value_named[i])
+              value_pair[i][n][e / 2] &= e & 1 ? 0x0000ffff : (int)0xffff0000;
+    }
+    to += (KEYS + step * S::CHANNELS) * 1024;
+#pragma unroll
+    for (int n = 0; n < S::UNITS; ++n) {
+      const Kv4Values<D> values(value[0][n], value[1][n], value_pair[0][n], value_pair[1][n], lane);
+#pragma unroll
+      for (int k = 0; k < S::NIBBLES / 2; ++k) {
+        const int pair = n * (S::NIBBLES / 2) + k;
+        if (pair / VALUE_EACH != value_part) continue;
+        v8h even, odd;
+        values.pair(k, even, odd);
+        *reinterpret_cast<v8h *>(to + (2 * pair) * 1024) = even;
+        *reinterpret_cast<v8h *>(to + (2 * pair + 1) * 1024) = odd;
+      }
+    }
+  };
+
+  if (tiles > 0) {
+    fetch(0);
+    unpack(0);
+  }
+  if (tiles > 1) fetch(1);
+  __syncthreads();
+  for (int tile = 0; tile < tiles; ++tile) {
+    const int stage = tile & 1, token = begin + tile * TILE;
+    if (tile + 1 < tiles) unpack(stage ^ 1);
+    if (tile + 2 < tiles) fetch(tile + 2);
+    if (token < most) {
+      const uint8_t *from = smem + stage * STAGE + 16 * lane;
+      v4f score[RT][2][2];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) score[t][u / 2][u % 2] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < S::KEY_STEPS; ++i) {
+          const v8h k = *reinterpret_cast<const v8h *>(from + (u * S::KEY_STEPS + i) * 1024);
+#pragma unroll
+          for (int t = 0; t < RT; ++t) score[t][u / 2][u % 2] = multiply(k, q[t][i], score[t][u / 2][u % 2]);
+        }
+      }
+      const v4i all_named = *reinterpret_cast<const v4i *>(named[stage]);
+      if (token + TILE > fewest || !__builtin_amdgcn_readfirstlane(all_named[0] & all_named[1] & all_named[2] & all_named[3])) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+              if (token + 16 * u + 4 * h + e >= sees[t] || !all_named[u]) score[t][u / 2][u % 2][e] = -__builtin_inff();
+      }
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        v8h p[RT];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) p[t] = weights(score[t][half], scale[t], top[t], total[t], out[t], h);
+#pragma unroll
+        for (int j = 0; j < S::CHANNELS; ++j) {
+          const v8h v = *reinterpret_cast<const v8h *>(from + (KEYS + half * S::CHANNELS + j) * 1024);
+#pragma unroll
+          for (int t = 0; t < RT; ++t) out[t][j] = multiply(p[t], v, out[t][j]);
+        }
+      }
+    }
+    __syncthreads();
+  }
+
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    float all = total[t];
+    all += __shfl_xor(all, 16);
+    all += __shfl_xor(all, 32);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int row = wave_row + 16 * t + 4 * h + e;
+      const float l = __shfl(all, 4 * h + e), m = __shfl(top[t], 4 * h + e);
+      if (row >= rows) continue;
+      const int query = row / P.shared, within = row - query * P.shared;
+      const float by = P.partials ? 1.0f : (l != 0.0f ? 1.0f / l : 0.0f);  // (a row that sees nothing: zeros)
+      const int64_t at = (req.q0 + query) * P.ldo + (int64_t)(head * P.shared + within) * D;
+      float *to = nullptr;
+      if (P.partials) {
+        const int64_t row_of_all = ((req.q0 + query) * P.kv_heads + head) * P.shared + within;
+        to = P.partials + (row_of_all * P.ranges + range) * PARTIAL<D>;
+        if (c == 0) *reinterpret_cast<v2f *>(to + D) = v2f{m, l};
+      }
+#pragma unroll
+      for (int j = 0; j < S::CHANNELS; j += 4) {
+        const v4f o = v4f{out[t][j][e], out[t][j + 1][e], out[t][j + 2][e], out[t][j + 3][e]} * by;
+        const int channel = S::value_channel(j / S::NIBBLES, j % S::NIBBLES, c);
+        if (P.partials) *reinterpret_cast<v4f *>(to + channel) = o;
+        else store_real4(P.O, at + channel, TYPE, o);
+      }
+    }
+  }
+}
+
+// The ranges of one row and head joined: a workgroup to a row, D / 4 lanes to a range, in turn.
+template <int D, int TYPE>
+__global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs P) {
+  constexpr int LANES = D / 4, GROUPS = 256 / LANES;
+  __shared__ v4f sums[GROUPS][LANES];
+  __shared__ float tops[GROUPS], totals[GROUPS];
+  const int at = threadIdx.x % LANES, group = threadIdx.x / LANES;
+  const int of_all = P.first + blockIdx.x, r = blockIdx.z;
+  const int head = of_all % (P.kv_heads * P.shared), query = of_all / (P.kv_heads * P.shared);
+  const Request req = request_of(P, r);
+  if (query >= req.queries) return;
+  const int seen = req.keys - req.queries + query + 1;
+  // (every range that the row's tile went through has written; those that hold none of the row's keys, a sum of zero)
+  const int ranges = seen <= 0 ? 1 : (seen + P.span - 1) / P.span;
+  const float *from = P.partials + ((req.q0 + query) * P.kv_heads * P.shared + head) * (int64_t)P.ranges * PARTIAL<D>;
+  float m = LOWEST, l = 0.0f;
+  v4f o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int i = group; i < ranges; i += GROUPS) {
+    const v2f ml = *reinterpret_cast<const v2f *>(from + (int64_t)i * PARTIAL<D> + D);
+    const v4f x = *reinterpret_cast<const v4f *>(from + (int64_t)i * PARTIAL<D> + 4 * at);
+    const float top = fmaxf(m, ml[0]), a = __builtin_amdgcn_exp2f(m - top), b = __builtin_amdgcn_exp2f(ml[0] - top);
+    o = o * a + x * b;
+    l = l * a + ml[1] * b;
+    m = top;
+  }
+  sums[group][at] = o;
+  if (at == 0) {
+    tops[group] = m;
+    totals[group] = l;
+  }
+  __syncthreads();
+  if (group > 0) return;
+#pragma unroll
+  for (int w = 1; w < GROUPS; ++w) {
+    const float top = fmaxf(m, tops[w]), a = __builtin_amdgcn_exp2f(m - top), b = __builtin_amdgcn_exp2f(tops[w] - top);
+    o = o * a + sums[w][at] * b;
+    l = l * a + totals[w] * b;
+    m = top;
+  }
+  store_real4(P.O, (req.q0 + query) * P.ldo + (int64_t)head * D + 4 * at, TYPE, o * (l != 0.0f ? 1.0f / l : 0.0f));
+}
+
+// `count` things, `each` workgroups to one, as many in a launch as a grid holds.
+hipError_t launch_in_slabs(void (*kernel)(AttentionArgs), AttentionArgs P, int64_t count, int64_t each, int requests,
+                           unsigned threads, size_t lds, hipStream_t s) {
+  const int64_t most = ((int64_t)1 << 22) / each > 0 ? ((int64_t)1 << 22) / each : 1;
+  for (int64_t i = 0; i < count; i += most) {
+    P.first = (int)i;
+    const int64_t here = count - i < most ? count - i : most;
+    const hipError_t e = launch_with(reinterpret_cast<const void *>(kernel), dim3((unsigned)(here * each), 1, (unsigned)requests),
+                                     threads, lds, s, &P);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+// How a call is cut: rows to a workgroup, and the keys into ranges of `span`.
+struct Cut {
+  bool tiles;  // the kernel for many rows
+  int rows, ranges, span;
+};
+Cut cut_call(int64_t requests, int64_t kv_heads, int64_t shared, int head_dim, int64_t max_q, int64_t max_kv) {
+  const int64_t rows = max_q * shared;
+  Cut cut;
+  cut.tiles = rows > 32;
+  cut.rows = rows <= 16 ? 16 : (rows <= 32 ? 32 : (rows <= 128 || head_dim == 256 ? 128 : 256));
+  const int64_t groups = requests * kv_heads * ((rows + cut.rows - 1) / cut.rows);
+  const int64_t round = cut.tiles ? 64 : WAVES * STEP;  // keys between two barriers, or of all waves' steps
+  int64_t want = ((cut.tiles ? 1 : 2) * compute_units() + groups - 1) / groups;
+  const int64_t least = cut.tiles ? 8 : 4;  // rounds to a range
+  const int64_t most = (max_kv + least * round - 1) / (least * round);
+  if (want > most) want = most;
+  if (want < 1) want = 1;
+  int64_t each = (max_kv + want - 1) / want;
+  each = (each + round - 1) / round * round;
+  if (each < round) each = round;
+  cut.span = (int)each;
+  cut.ranges = (int)((max_kv + each - 1) / each);
+  if (cut.ranges < 1) cut.ranges = 1;
+  return cut;
+}
+
+template <int D, int TYPE>
+hipError_t launch_for(const AttentionArgs &P, const Cut &cut, int requests, hipStream_t s) {
+  const int64_t rows = (int64_t)P.max_q * P.shared, groups = (rows + cut.rows - 1) / cut.rows * P.kv_heads;
+  constexpr int RT = D == 256 ? 1 : 2;  // (sixteen rows of 256 channels are as many registers as 32 of 128)
+  void (*kernel)(AttentionArgs);
+  unsigned threads = 256;
+  size_t lds = (size_t)WAVES * 16 * (D + 4) * 4;
+  if (cut.tiles) {
+    const bool eight = cut.rows == 128 * RT;
+    kernel = attention_tiles_kernel<D, TYPE, RT, 8>;
+    if constexpr (RT == 2) {
+      if (!eight) kernel = attention_tiles_kernel<D, TYPE, RT, 4>;
+    }
+    threads = eight ? 512 : 256;
+    lds = (size_t)(D / 4) * 2048;
+  } else {
+    kernel = cut.rows == 16 ? attention_rows_kernel<D, TYPE, 1> : attention_rows_kernel<D, TYPE, 2>;
+  }
+  hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(kernel), lds + 1024);  // (and what is not dynamic)
+  if (e == hipSuccess) e = launch_in_slabs(kernel, P, groups, P.ranges, requests, threads, lds, s);
+  if (e != hipSuccess || !P.partials) return e;
+  return launch_in_slabs(attention_join_kernel<D, TYPE>, P, (int64_t)P.max_q * P.kv_heads * P.shared, 1, requests, 256, 0, s);
+}
+
+}  // namespace
+
+size_t attention_scratch(int64_t requests, int64_t kv_heads, int64_t shared, int head_dim, int64_t max_q, int64_t max_kv) {
+  const int ranges = cut_call(requests, kv_heads, shared, head_dim, max_q, max_kv).ranges;
+  return ranges > 1 ? (size_t)(requests * max_q * kv_heads * shared) * (size_t)ranges * (size_t)(head_dim + 4) * 4 + 16 : 0;
+}
+
+hipError_t launch_attention(AttentionArgs P, int requests, int head_dim, int type, void *ws, size_t ws_bytes, hipStream_t s) {
+  const Cut cut = cut_call(requests, P.kv_heads, P.shared, head_dim, P.max_q, P.max_kv);
+  P.ranges = cut.ranges;
+  P.span = cut.span;
+  const size_t skip = (16 - reinterpret_cast<uintptr_t>(ws) % 16) % 16;
+  const size_t need = (size_t)P.q_rows * (size_t)(P.kv_heads * P.shared) * (size_t)P.ranges * (size_t)(head_dim + 4) * 4;
+  if (P.ranges > 1 && ws && ws_bytes >= skip && ws_bytes - skip >= need) {
+    P.partials = reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + skip);
+  } else {
+    P.partials = nullptr;
+    P.ranges = 1;
+    P.span = 0;
+  }
+  // (requests go to grid.z)
+  const int most = 65535;
+  for (int r = 0; r < requests; r += most) {
+    AttentionArgs A = P;
+    A.q_starts += r;
+    A.kv_lengths += r;
+    A.block_table += (int64_t)r * P.table_stride;
+    const int here = requests - r < most ? requests - r : most;
+    hipError_t e;
+    if (type == REAL_BF16)
+      e = head_dim == 64    ? launch_for<64, REAL_BF16>(A, cut, here, s)
+          : head_dim == 128 ? launch_for<128, REAL_BF16>(A, cut, here, s)
+                            : launch_for<256, REAL_BF16>(A, cut, here, s);
+    else
+      e = head_dim == 64    ? launch_for<64, REAL_F16>(A, cut, here, s)
+          : head_dim == 128 ? launch_for<128, REAL_F16>(A, cut, here, s)
+                            : launch_for<256, REAL_F16>(A, cut, here, s);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace mip

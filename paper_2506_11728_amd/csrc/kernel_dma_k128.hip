@@ -78,9 +78,21 @@ hipError_t launch_for(const Problem &p, hipStream_t s, unsigned long long *clock
   else if (b_kc) MIP_PICK(false, true);
   else MIP_PICK(false, false);
 #undef MIP_PICK
-  hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(kern), lds);
+  const void *kernel = reinterpret_cast<const void *>(kern), *args = &P;
+  DmaLinearK128Params PL;
+  if (p.linear) {
+    static_cast<DmaParams &>(PL) = P;
+    PL.linear = *p.linear;
+    args = &PL;
+    void (*linear)(DmaLinearK128Params) =
+        BM == DM && (p.m % DM || p.n % DN) ? dma128_kernel<DM, DN, true, true, LINEAR_OUT, true>
+        : b_kc                             ? dma128_kernel<BM, BN, true, true, LINEAR_OUT>
+                                           : dma128_kernel<BM, BN, true, false, LINEAR_OUT>;
+    kernel = reinterpret_cast<const void *>(linear);
+  }
+  hipError_t e = allow_dynamic_lds(kernel, lds);
   if (e != hipSuccess) return e;
-  return launch_with(reinterpret_cast<const void *>(kern), grid, NTHREADS, lds, s, &P);
+  return launch_with(kernel, grid, NTHREADS, lds, s, args);
 }
 
 }  // namespace

@@ -1,0 +1,184 @@
+// Rows of real numbers brought to 8 bits, each with a scale of its own, optionally through an RMS norm:
+//     z_j = x_j w_j (w_j = 1 without a norm),  a = max_j |z_j|,  q_j = rint(127 z_j / a),
+//     scale = a / 127, times 1 / sqrt(mean_j x_j^2 + eps) with a norm.
+// The norm's factor is the same in every z_j and in a, so it never meets q_j: the codes do not depend on
+// the order in which the squares are summed.
+//
+// Bound by memory: x is read once, a byte an element written.  A row stays in the registers of its workgroup
+// between the reduction and the rounding where it fits (16384 numbers); longer rows are read a second time,
+// through the cache.  A wave to a row up to 1024 columns, four waves up to 16384, sixteen beyond.
+#include "layer_internal.h"
+#include "real.h"
+
+namespace mip {
+
+namespace {
+
+struct QuantizeParams {
+  const void *X;
+  int64_t ldx, rows, cols;
+  const float *weight;  // null: no norm
+  float eps;
+  int8_t *Q;
+  int64_t ldq;
+  float *scales;
+};
+
+struct __attribute__((packed, aligned(1))) byte_oct { uint64_t v; };
+
+template <typename T>
+struct real_of;
+template <> struct real_of<float> { static constexpr int type = REAL_F32; };
+template <> struct real_of<__bf16> { static constexpr int type = REAL_BF16; };
+template <> struct real_of<_Float16> { static constexpr int type = REAL_F16; };
+
+// x_j and w_j of eight columns from j on; what lies behind the row is zero.
+template <typename T>
+__device__ __forceinline__ void load_oct(const QuantizeParams &P, int64_t row, int64_t j, float (&x)[8]) {
+  constexpr int TYPE = real_of<T>::type;
+  if (j + 8 <= P.cols) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const v4f v = load_real4(P.X, row * P.ldx + j + 4 * h, TYPE);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[4 * h + e] = v[e];
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = j + e < P.cols ? load_real(P.X, row * P.ldx + j + e, TYPE) : 0.0f;
+  }
+}
+__device__ __forceinline__ void times_weight(const QuantizeParams &P, int64_t j, float (&x)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (j + e < P.cols) x[e] = __fmul_rn(x[e], P.weight[j + e]);
+}
+
+// The quotient num / a for |num| <= 127 a, correctly rounded: the reciprocal r of a is, and one step of
+// Newton's iteration on the quotient then is as well (Markstein's theorem), where nothing underflows.
+__device__ __forceinline__ int code_of(float z, float a, float r) {
+  const float num = __fmul_rn(z, 127.0f);
+  const float q = num * r;
+  return (int)__builtin_rintf(__builtin_fmaf(__builtin_fmaf(-q, a, num), r, q));
+}
+
+// WAVES to a row, ROWS rows to a workgroup; HELD: eights of columns a thread keeps, 0: none.
+template <typename T, int WAVES, int ROWS, int HELD>
+__global__ __launch_bounds__(64 * WAVES *ROWS) void quantize_kernel(QuantizeParams P) {
+  constexpr int THREADS = 64 * WAVES;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64 % WAVES, at = threadIdx.x % THREADS;
+  const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS;
+  const bool here = row < P.rows;
+  float x[HELD ? HELD : 1][8];
+  float top = 0.0f, squares = 0.0f;
+  auto take = [&](int64_t j, float (&v)[8]) {
+    load_oct<T>(P, row, j, v);
+    if (P.weight) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) squares += v[e] * v[e];
+      times_weight(P, j, v);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float m = fabsf(v[e]);
+      top = m <= top || top != top ? top : m;  // (a NaN stays)
+    }
+  };
+  if (HELD) {
+#pragma unroll
+    for (int u = 0; u < HELD; ++u) {
+      const int64_t j = 8 * ((int64_t)u * THREADS + at);
+      if (here && j < P.cols) take(j, x[u]);
+    }
+  } else if (here) {
+    for (int64_t j = 8 * at; j < P.cols; j += 8 * THREADS) take(j, x[0]);
+  }
+  auto larger = [](float a, float b) { return a != a ? a : (b <= a ? a : b); };
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    top = larger(top, __shfl_xor(top, d));
+    squares += __shfl_xor(squares, d);
+  }
+  if constexpr (WAVES > 1) {
+    __shared__ float both[2][WAVES];
+    if (lane == 0) {
+      both[0][wave] = top;
+      both[1][wave] = squares;
+    }
+    __syncthreads();
+    top = both[0][0];
+    squares = both[1][0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) {
+      top = larger(top, both[0][w]);
+      squares += both[1][w];
+    }
+  }
+  if (!here) return;
+  const bool finite = top < __builtin_inff();  // (false for a NaN)
+  if (at == 0) {
+    float scale = finite ? __fdiv_rn(top, 127.0f) : __builtin_nanf("");
+    if (P.weight) scale *= __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(squares, (float)P.cols) + P.eps));
+    P.scales[row] = scale;
+  }
+  // far from 1, a power of two keeps the reciprocal and the products in range, and changes no quotient
+  const float by = top < 0x1p-60f ? 0x1p60f : (top > 0x1p60f ? 0x1p-60f : 1.0f);
+  const float a = top * by, r = finite && top > 0.0f ? __fdiv_rn(1.0f, a) : 0.0f;
+  auto put = [&](int64_t j, float (&v)[8]) {
+    uint64_t word = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) word |= (uint64_t)(uint8_t)(r != 0.0f ? code_of(v[e] * by, a, r) : 0) << (8 * e);
+    int8_t *q = P.Q + row * P.ldq + j;
+    if (j + 8 <= P.cols) {
+      reinterpret_cast<byte_oct *>(q)->v = word;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 7; ++e)
+        if (j + e < P.cols) q[e] = (int8_t)(word >> (8 * e));
+    }
+  };
+  if (HELD) {
+#pragma unroll
+    for (int u = 0; u < HELD; ++u) {
+      const int64_t j = 8 * ((int64_t)u * THREADS + at);
+      if (j < P.cols) put(j, x[u]);
+    }
+  } else {
+    for (int64_t j = 8 * at; j < P.cols; j += 8 * THREADS) {
+      load_oct<T>(P, row, j, x[0]);
+      if (P.weight) times_weight(P, j, x[0]);
+      put(j, x[0]);
+    }
+  }
+}
+
+template <typename T>
+hipError_t launch_for(const QuantizeParams &P, hipStream_t s) {
+  void (*kernel)(QuantizeParams);
+  unsigned threads = 256;
+  int64_t rows = 1;
+  if (P.cols <= 1024) { kernel = quantize_kernel<T, 1, 4, 2>; rows = 4; }
+  else if (P.cols <= 4096) kernel = quantize_kernel<T, 4, 1, 2>;
+  else if (P.cols <= 16384) kernel = quantize_kernel<T, 4, 1, 8>;
+  else { kernel = quantize_kernel<T, 16, 1, 0>; threads = 1024; }
+  const dim3 grid((unsigned)((P.rows + rows - 1) / rows));
+  return launch_with(reinterpret_cast<const void *>(kernel), grid, threads, 0, s, &P);
+}
+
+}  // namespace
+
+hipError_t launch_quantize(int64_t rows, int64_t cols, const void *X, int64_t ldx, int type, const float *weight, float eps,
+                           int8_t *Q, int64_t ldq, float *scales, hipStream_t s) {
+  // (a grid has at most 2^32 - 1 threads a dimension: taller matrices in slabs)
+  const int64_t slab = (int64_t)1 << 22;
+  for (int64_t i = 0; i < rows; i += slab) {
+    const QuantizeParams P{static_cast<const uint8_t *>(X) + i * ldx * real_bytes(type), ldx,
+                           rows - i < slab ? rows - i : slab, cols, weight, eps, Q + i * ldq, ldq, scales + i};
+    const hipError_t e = type == REAL_F32 ? launch_for<float>(P, s)
+                         : type == REAL_BF16 ? launch_for<__bf16>(P, s) : launch_for<_Float16>(P, s);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace mip

@@ -1,6 +1,7 @@
 // Layout-agnostic kernels: the zero fill for k == 0 and a one-thread-per-element
 // GEMM that accepts any strides and alignments.  The latter is the path of last
 // resort and the in-library cross-check for the MFMA kernels; it is slow.
+#include "linear.h"
 #include "mip_internal.h"
 
 namespace mip {
@@ -15,7 +16,17 @@ __global__ __launch_bounds__(256) void fill_zero_kernel(int32_t *__restrict__ C,
 
 // C(i,j) (+)= sum_p A(i,p) * B(p,j): the definition of the MIP GEMM (paper
 // Section 5: INT8 products accumulated in INT32), one output element per thread.
-__global__ __launch_bounds__(256) void simple_kernel(Problem p) {
+struct SimpleLinearParams {
+  Problem p;
+  LinearArgs linear;
+  int64_t row0;  // of this launch's first row in C
+};
+template <bool LINEAR>
+__global__ __launch_bounds__(256) void simple_kernel(std::conditional_t<LINEAR, SimpleLinearParams, Problem> args) {
+  const Problem p = [&] {
+    if constexpr (LINEAR) return args.p;
+    else return args;
+  }();
   const int64_t j = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
   const int64_t i = (int64_t)blockIdx.y * 4 + (threadIdx.x >> 6);
   if (i >= p.m || j >= p.n) return;
@@ -28,6 +39,10 @@ __global__ __launch_bounds__(256) void simple_kernel(Problem p) {
     if (!p.a_unsigned) av = (uint32_t)(int32_t)(int8_t)av;
     if (!p.b_unsigned) bv = (uint32_t)(int32_t)(int8_t)bv;
     acc += av * bv;
+  }
+  if constexpr (LINEAR) {
+    linear_one(args.linear, args.row0 + i, j, (int)acc);
+    return;
   }
   if (p.out_float == 2) {  // requantised int8 output: clip(rint(float(sum) * scale))
     float r = __builtin_rintf(__fmul_rn((float)(int32_t)acc, p.scale));
@@ -74,7 +89,8 @@ hipError_t launch_simple(const Problem &p, hipStream_t s) {
     q.C = p.out_float == 2 ? reinterpret_cast<int32_t *>(reinterpret_cast<int8_t *>(p.C) + i0 * p.ldc)
                            : p.C + i0 * p.ldc;
     dim3 grid = grid_for(q.m, q.n, q.batch);
-    hipLaunchKernelGGL(simple_kernel, grid, dim3(256), 0, s, q);
+    if (p.linear) hipLaunchKernelGGL(simple_kernel<true>, grid, dim3(256), 0, s, SimpleLinearParams{q, *p.linear, i0});
+    else hipLaunchKernelGGL(simple_kernel<false>, grid, dim3(256), 0, s, q);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

@@ -29,6 +29,7 @@
 // k contiguous, n a multiple of 16, k a multiple of 64, 16-byte aligned operand
 // bases and leading dimensions.
 #include "dma_common.h"
+#include "linear.h"
 
 namespace mip {
 
@@ -67,6 +68,10 @@ struct SlabParams {
   float scale;
 };
 
+struct SlabLinearParams : SlabParams {
+  LinearArgs linear;
+};
+
 template <int N>
 __device__ __forceinline__ void loads_landed() {  // all but the N newest direct loads
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
@@ -78,9 +83,10 @@ __device__ __forceinline__ int kc_chunk(int q, int lane) { return (lane & 7) ^ (
 
 // MT: row blocks of 16 (m <= 16 * MT).  NT: column blocks of 16 per workgroup.
 // B_KC: B stored with k contiguous (column-major).  UNS: 0 both signed, 1 A
-// unsigned, 2 B unsigned.
+// unsigned, 2 B unsigned; LINEAR_OUT: both signed, the write-back of a linear layer.
 template <int MT, int NT, bool B_KC, int UNS, Rings RINGS>
-__global__ __launch_bounds__(64 * slab_waves(MT, NT, RINGS)) void slab_kernel(SlabParams P) {
+__global__ __launch_bounds__(64 * slab_waves(MT, NT, RINGS)) void slab_kernel(
+    std::conditional_t<UNS == LINEAR_OUT, SlabLinearParams, SlabParams> P) {
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   constexpr int W = slab_waves(MT, NT, RINGS), DA = steps_of_a(MT, NT, RINGS), DB = steps_of_b(MT, NT, RINGS);
   static_assert(DB >= DA, "the waits below");
@@ -287,6 +293,14 @@ __global__ __launch_bounds__(64 * slab_waves(MT, NT, RINGS)) void slab_kernel(Sl
     const int b = wave + W * i;
     if (b >= BLOCKS) break;
     const int mt = b / NT, nt = b % NT;
+    if constexpr (UNS == LINEAR_OUT) {
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int row = 16 * mt + 4 * (lane >> 4) + v;
+        if (row < P.m) linear_one(P.linear, row, n0 + 16 * nt + (lane & 15), sums[i][v]);
+      }
+      continue;
+    }
     int32_t *c = P.C + n0 + 16 * nt + (lane & 15);
     // (an accumulating call reads its four old words before the first store, not one behind each)
     int old[4] = {0, 0, 0, 0};
@@ -309,6 +323,11 @@ void (*pick(bool b_kc, int uns))(SlabParams) {
                             : (uns == 1 ? slab_kernel<MT, NT, true, 1, RINGS> : slab_kernel<MT, NT, true, 2, RINGS>);
   return uns == 0 ? slab_kernel<MT, NT, false, 0, RINGS>
                   : (uns == 1 ? slab_kernel<MT, NT, false, 1, RINGS> : slab_kernel<MT, NT, false, 2, RINGS>);
+}
+
+template <int MT, int NT, Rings RINGS = DEEP>
+void (*pick_linear(bool b_kc))(SlabLinearParams) {
+  return b_kc ? slab_kernel<MT, NT, true, LINEAR_OUT, RINGS> : slab_kernel<MT, NT, false, LINEAR_OUT, RINGS>;
 }
 
 }  // namespace
@@ -345,25 +364,51 @@ hipError_t launch_slab(const Problem &p, int nt, hipStream_t s) {
   P.scale = p.scale;
   const int uns = p.a_unsigned ? 1 : (p.b_unsigned ? 2 : 0);
   const int mt = p.m <= 16 ? 1 : (p.m <= 32 ? 2 : 4);
-  void (*kern)(SlabParams) = nullptr;
   const bool many = P.tiles > compute_units(), few_steps = P.nsteps <= 4;
   Rings rings = DEEP;
   if (nt == 1 && mt == 1) rings = few_steps || (many && P.nsteps < 16) ? FEW : (many ? HALF : DEEP);
   else if ((nt == 4 && mt == 1) || (nt == 1 && mt == 2)) rings = many || few_steps ? FEW : DEEP;
-  if (rings == HALF) kern = pick<1, 1, HALF>(b_kc, uns);
-  else if (rings == FEW && nt == 4) kern = pick<1, 4, FEW>(b_kc, uns);
-  else if (rings == FEW) kern = mt == 1 ? pick<1, 1, FEW>(b_kc, uns) : pick<2, 1, FEW>(b_kc, uns);
-  else if (nt == 1) kern = mt == 1 ? pick<1, 1>(b_kc, uns) : (mt == 2 ? pick<2, 1>(b_kc, uns) : pick<4, 1>(b_kc, uns));
-  else if (nt == 2) kern = mt == 1 ? pick<1, 2>(b_kc, uns) : (mt == 2 ? pick<2, 2>(b_kc, uns) : pick<4, 2>(b_kc, uns));
-  else kern = mt == 1 ? pick<1, 4>(b_kc, uns) : (mt == 2 ? pick<2, 4>(b_kc, uns) : pick<4, 4>(b_kc, uns));
+#define MIP_PICK(CALL)                                                                            \
+  if (rings == HALF) CALL(1, 1, HALF);                                                            \
+  else if (rings == FEW && nt == 4) CALL(1, 4, FEW);                                              \
+  else if (rings == FEW && mt == 1) CALL(1, 1, FEW);                                              \
+  else if (rings == FEW) CALL(2, 1, FEW);                                                         \
+  else if (nt == 1 && mt == 1) CALL(1, 1, DEEP);                                                  \
+  else if (nt == 1 && mt == 2) CALL(2, 1, DEEP);                                                  \
+  else if (nt == 1) CALL(4, 1, DEEP);                                                             \
+  else if (nt == 2 && mt == 1) CALL(1, 2, DEEP);                                                  \
+  else if (nt == 2 && mt == 2) CALL(2, 2, DEEP);                                                  \
+  else if (nt == 2) CALL(4, 2, DEEP);                                                             \
+  else if (mt == 1) CALL(1, 4, DEEP);                                                             \
+  else if (mt == 2) CALL(2, 4, DEEP);                                                             \
+  else CALL(4, 4, DEEP)
+  const void *kernel, *args = &P;
+  SlabLinearParams PL;
+  if (p.linear) {
+    static_cast<SlabParams &>(PL) = P;
+    PL.linear = *p.linear;
+    args = &PL;
+    void (*linear)(SlabLinearParams) = nullptr;
+#define MIP_LINEAR(MT, NT, RINGS) linear = pick_linear<MT, NT, RINGS>(b_kc)
+    MIP_PICK(MIP_LINEAR);
+#undef MIP_LINEAR
+    kernel = reinterpret_cast<const void *>(linear);
+  } else {
+    void (*kern)(SlabParams) = nullptr;
+#define MIP_PLAIN(MT, NT, RINGS) kern = pick<MT, NT, RINGS>(b_kc, uns)
+    MIP_PICK(MIP_PLAIN);
+#undef MIP_PLAIN
+    kernel = reinterpret_cast<const void *>(kern);
+  }
+#undef MIP_PICK
   const int waves = slab_waves(mt, nt, rings);
   const size_t lds = (size_t)waves * 2048 * (steps_of_b(mt, nt, rings) * nt + steps_of_a(mt, nt, rings) * mt);
   {
-    hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(kern), lds);
+    hipError_t e = allow_dynamic_lds(kernel, lds);
     if (e != hipSuccess) return e;
   }
   dim3 grid((unsigned)(((P.tiles + 7) / 8) * 8));
-  return launch_with(reinterpret_cast<const void *>(kern), grid, 64 * waves, lds, s, &P);
+  return launch_with(kernel, grid, 64 * waves, lds, s, args);
 }
 
 }  // namespace mip

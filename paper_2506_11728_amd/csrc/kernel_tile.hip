@@ -27,6 +27,7 @@
 // adds 128 * sum_p y(p) of the other (signed) operand, which the waves
 // accumulate from the fragments they already hold.  Exact modulo 2^32.
 #include "dma_common.h"
+#include "linear.h"
 
 namespace mip {
 
@@ -37,8 +38,12 @@ struct TileParams {
   int atomic;        // several workgroups add into the same tile of C (split k)
 };
 
-template <int BM, int BN, bool A_KC, bool B_KC>
-__global__ __launch_bounds__(NTHREADS) void tile_kernel(TileParams tp) {
+struct TileLinearParams : TileParams {
+  LinearArgs linear;
+};
+
+template <int BM, int BN, bool A_KC, bool B_KC, bool LINEAR = false>
+__global__ __launch_bounds__(NTHREADS) void tile_kernel(std::conditional_t<LINEAR, TileLinearParams, TileParams> tp) {
   constexpr int FM = BM / 64, FN = BN / 64;  // 32 x 32 blocks per wave, down and across
   using SA = Stage<BM, A_KC>;
   using SB = Stage<BN, B_KC>;
@@ -155,6 +160,14 @@ __global__ __launch_bounds__(NTHREADS) void tile_kernel(TileParams tp) {
   // ---- epilogue: unsigned-operand correction, then C = acc or C += acc ----
   unsigned_correction<FM, FN>(acc, sumA, sumB, flipA != 0, flipB != 0, lane);
   const int64_t mw = m0 + wm * (BM / 2), nw = n0 + wn * (BN / 2);  // the wave's sub-tile
+  if constexpr (LINEAR) {
+    // the k loop ended on a workgroup barrier: no wave still reads the stages
+    int32_t *patch = reinterpret_cast<int32_t *>(smem + wave * STORE_PATCH_BYTES);
+    if (!edge_tile) store_linear32<FM, FN, true>(acc, tp.linear, mw, nw, p.m - mw, p.n - nw, lane, patch);
+    else if (mw < p.m && nw < p.n)
+      store_linear32<FM, FN, false>(acc, tp.linear, mw, nw, p.m - mw, p.n - nw, lane, patch);
+    return;
+  }
   if (mw < p.m && nw < p.n) {
     if (p.out_float == 2) {  // int8 output: C is a matrix of bytes
       int8_t *Q = reinterpret_cast<int8_t *>(p.C) + mw * p.ldc + nw;
@@ -204,6 +217,13 @@ static hipError_t launch_cfg(const Problem &p, int splits, hipStream_t s) {
   const int ntiles = (int)(tiles_m * tiles_n);
   dim3 grid((unsigned)(((ntiles + 7) / 8) * 8), (unsigned)splits, (unsigned)p.batch);
   const bool a_kc = p.a_sk == 1, b_kc = p.b_sk == 1;
+  if (p.linear) {
+    TileLinearParams tl;
+    static_cast<TileParams &>(tl) = tp;
+    tl.linear = *p.linear;
+    void (*linear)(TileLinearParams) = b_kc ? tile_kernel<BM, BN, true, true, true> : tile_kernel<BM, BN, true, false, true>;
+    return launch_with(reinterpret_cast<const void *>(linear), grid, NTHREADS, 0, s, &tl);
+  }
   void (*kern)(TileParams) = a_kc ? (b_kc ? tile_kernel<BM, BN, true, true> : tile_kernel<BM, BN, true, false>)
                                   : (b_kc ? tile_kernel<BM, BN, false, true> : tile_kernel<BM, BN, false, false>);
   return launch_with(reinterpret_cast<const void *>(kern), grid, NTHREADS, 0, s, &tp);

@@ -1,0 +1,198 @@
+// Write-back of a linear layer on 8-bit operands: from the int32 sums S of the product to
+//     C(i, j) = act( float(S(i, j)) * row_scale(i) * col_scale(j) + bias(j) ) + R(i, j)
+// in float32, rounded once to the type of C.  Shared by the MFMA kernels, whose LINEAR forms
+// (UNS == LINEAR_OUT) differ from the others in nothing else: the sums are complete before anything
+// is converted, in integers, and what the write-back adds to a product is the traffic of R and of
+// C, which in 16 bits is half that of int32 sums.
+#pragma once
+#include "epilogue16.h"
+#include "mip_internal.h"
+#include "real.h"
+
+namespace mip {
+
+constexpr int LINEAR_OUT = 5;  // the kernels' UNS parameter: both operands signed, this write-back
+
+// The activations fall into three kinds, by how much code they are; the write-back loops are
+// instantiated once per kind and entered through a wave-uniform switch.
+//   0: max(y, floor), floor 0 or -infinity
+//   1: y / (1 + exp(-y (c1 + c3 y^2))): SiLU, and GELU's tanh form, since (1 + tanh u) / 2 = 1 / (1 + exp(-2 u))
+//   2: y * erfc(-y / sqrt 2) / 2: GELU
+template <int KIND>
+struct Activate {
+  float c1, c3;  // kind 0: the floor in c1
+  __device__ static __forceinline__ Activate of(int act) {
+    if (KIND == 0) return {act == ACT_RELU ? 0.0f : -__builtin_inff(), 0.0f};
+    const float c = 1.5957691216057308f;  // 2 sqrt(2 / pi)
+    if (act == ACT_GELU_TANH) return {c, c * 0.044715f};
+    return {1.0f, 0.0f};
+  }
+  __device__ __forceinline__ float operator()(float y) const {
+    if (KIND == 0) return y < c1 ? c1 : y;  // (a NaN stays one)
+    if (KIND == 1) {
+      const float t = y * (c1 + c3 * y * y);
+      // (at the far negative end exp overflows to infinity and the quotient is -0)
+      return y * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * t));
+    }
+    // erfc(z) for z >= 0 within 1.2e-7 of its value: t exp(-z^2 + P(t)), t = 1 / (1 + z / 2), the
+    // Chebyshev fit of Press et al., Numerical Recipes, section 6.2
+    const float z = fabsf(y) * 0.70710678118654752f;
+    const float t = __builtin_amdgcn_rcpf(1.0f + 0.5f * z);
+    float p = 0.17087277f;
+    p = p * t - 0.82215223f;
+    p = p * t + 1.48851587f;
+    p = p * t - 1.13520398f;
+    p = p * t + 0.27886807f;
+    p = p * t - 0.18628806f;
+    p = p * t + 0.09678418f;
+    p = p * t + 0.37409196f;
+    p = p * t + 1.00002368f;
+    p = p * t - 1.26551223f;
+    const float half = 0.5f * t * __builtin_amdgcn_exp2f(1.4426950408889634f * (p - z * z));  // erfc(z) / 2
+    return y * (y < 0.0f ? half : 1.0f - half);
+  }
+};
+__device__ __forceinline__ int activation_kind(int act) { return act == ACT_GELU ? 2 : (act >= ACT_GELU_TANH ? 1 : 0); }
+
+// The same roundings in every kernel: a result does not depend on which of them serves a call.
+__device__ __forceinline__ float linear_value(int sum, float row_scale, float col_scale, float bias) {
+  return __builtin_fmaf(__fmul_rn((float)sum, row_scale), col_scale, bias);
+}
+
+// Scales and biases of a lane's four columns, `count` of which exist.
+struct LinearColumns {
+  v4f scale, bias;
+};
+__device__ __forceinline__ LinearColumns linear_columns(const LinearArgs &L, int64_t col, int64_t count) {
+  LinearColumns c{{1.0f, 1.0f, 1.0f, 1.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (e < count && L.col_scale) c.scale[e] = L.col_scale[col + e];
+    if (e < count && L.bias) c.bias[e] = L.bias[col + e];
+  }
+  return c;
+}
+
+__device__ __forceinline__ v4f linear_residual(const LinearArgs &L, int64_t row, int64_t col, int64_t count) {
+  if (count >= 4) return load_real4(L.R, row * L.ldr + col, L.type);
+  v4f r = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (e < count) r[e] = load_real(L.R, row * L.ldr + col + e, L.type);
+  return r;
+}
+
+template <int KIND>
+__device__ __forceinline__ void linear_quad(const LinearArgs &L, const Activate<KIND> act, const LinearColumns &c,
+                                            int64_t row, int64_t col, int64_t count, v4i sum, float row_scale, v4f residual) {
+  v4f y;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = act(linear_value(sum[e], row_scale, c.scale[e], c.bias[e])) + residual[e];
+  if (count >= 4) {
+    store_real4(L.C, row * L.ldc + col, L.type, y);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < count) store_real(L.C, row * L.ldc + col + e, L.type, y[e]);
+  }
+}
+
+// One element, for the kernels that write C element by element.
+__device__ __forceinline__ void linear_one(const LinearArgs &L, int64_t row, int64_t col, int sum) {
+  float y = linear_value(sum, L.row_scale ? L.row_scale[row] : 1.0f, L.col_scale ? L.col_scale[col] : 1.0f,
+                         L.bias ? L.bias[col] : 0.0f);
+  switch (activation_kind(L.act)) {
+    case 0: y = Activate<0>::of(L.act)(y); break;
+    case 1: y = Activate<1>::of(L.act)(y); break;
+    default: y = Activate<2>::of(L.act)(y); break;
+  }
+  if (L.R) y += load_real(L.R, row * L.ldr + col, L.type);
+  store_real(L.C, row * L.ldc + col, L.type, y);
+}
+
+// The sums of PASSES row pieces of four columns, in LDS at patch + (t * ROWS + r0) * PITCH + c0,
+// written to rows row + t * ROWS.  The residuals and the row scales are on their way before the
+// first of them is used.
+template <int KIND, int PASSES, int ROWS, int PITCH, bool FULL>
+__device__ __forceinline__ void linear_pieces(const LinearArgs &L, const Activate<KIND> act, const LinearColumns &columns,
+                                              int64_t row, int64_t rows, int64_t col, int64_t count, const int32_t *patch) {
+  v4f residual[PASSES];
+  float row_scale[PASSES];
+  v4i sum[PASSES];
+#pragma unroll
+  for (int t = 0; t < PASSES; ++t) {
+    const bool here = (FULL || t * ROWS < rows) && count > 0;
+    residual[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    if (here && L.R) residual[t] = linear_residual(L, row + t * ROWS, col, count);
+    row_scale[t] = here && L.row_scale ? L.row_scale[row + t * ROWS] : 1.0f;
+    sum[t] = *reinterpret_cast<const v4i *>(patch + t * ROWS * PITCH);
+  }
+#pragma unroll
+  for (int t = 0; t < PASSES; ++t)
+    if ((FULL || t * ROWS < rows) && count > 0)
+      linear_quad<KIND>(L, act, columns, row + t * ROWS, col, count, sum[t], row_scale[t], residual[t]);
+}
+
+// Blocks of v_mfma_i32_16x16x64_i8 (epilogue16.h), sixteen rows at a time through the wave's patch.
+// row0, col0: the first element of the sub-tile in C; rows, cols: how much of it lies inside.
+template <int FM, int FN, int KIND, bool FULL>
+__device__ __forceinline__ void store_linear16_as(const v4i (&acc)[FM][FN], const LinearArgs &L, int64_t row0, int64_t col0,
+                                                  int64_t rows, int64_t cols, int lane, int32_t *patch) {
+  constexpr int PITCH = Patch16<FN>::PITCH, LANES_PER_ROW = 4 * FN, ROWS = 64 / LANES_PER_ROW, PASSES = 16 / ROWS;
+  const bool active = 64 % LANES_PER_ROW == 0 || lane < ROWS * LANES_PER_ROW;
+  const int r0 = active ? lane / LANES_PER_ROW : 0, c0 = 4 * (lane % LANES_PER_ROW);
+  const int64_t count = !active ? 0 : (FULL ? 4 : cols - c0);
+  const LinearColumns columns = linear_columns(L, col0 + c0, count);
+  const Activate<KIND> act = Activate<KIND>::of(L.act);
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+    if (!FULL && i * 16 >= rows) break;  // wave-uniform
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+      *reinterpret_cast<v4i *>(patch + (lane & 15) * PITCH + 16 * j + 4 * (lane >> 4)) = acc[i][j];
+    // same wave wrote and reads: LDS operations of a wave complete in order
+    if (64 % LANES_PER_ROW != 0) asm volatile("" ::: "memory");
+    linear_pieces<KIND, PASSES, ROWS, PITCH, FULL>(L, act, columns, row0 + i * 16 + r0, rows - (i * 16 + r0), col0 + c0,
+                                                   count, patch + r0 * PITCH + c0);
+  }
+}
+
+// Blocks of v_mfma_i32_32x32x32_i8 (epilogue.h), one at a time through the wave's STORE_PATCH_BYTES of LDS.
+template <int FM, int FN, int KIND, bool FULL>
+__device__ __forceinline__ void store_linear32_as(const v16i (&acc)[FM][FN], const LinearArgs &L, int64_t row0, int64_t col0,
+                                                  int64_t rows, int64_t cols, int lane, int32_t *patch) {
+  const int r0 = lane >> 3, c0 = 4 * (lane & 7);
+  const Activate<KIND> act = Activate<KIND>::of(L.act);
+#pragma unroll
+  for (int j = 0; j < FN; ++j) {
+    if (!FULL && j * 32 >= cols) break;  // wave-uniform
+    const int64_t count = FULL ? 4 : cols - (j * 32 + c0);
+    const LinearColumns columns = linear_columns(L, col0 + j * 32 + c0, count);
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      if (!FULL && i * 32 >= rows) break;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<v4i *>(patch + (lane & 31) * 36 + 8 * q + 4 * (lane >> 5)) =
+            v4i{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+      linear_pieces<KIND, 4, 8, 36, FULL>(L, act, columns, row0 + i * 32 + r0, rows - (i * 32 + r0), col0 + j * 32 + c0, count,
+                                          patch + r0 * 36 + c0);
+    }
+  }
+}
+
+#define MIP_STORE_LINEAR(NAME, BLOCK)                                                                              \
+  template <int FM, int FN, bool FULL>                                                                             \
+  __device__ __forceinline__ void NAME(const BLOCK (&acc)[FM][FN], const LinearArgs &L, int64_t row0, int64_t col0, \
+                                       int64_t rows, int64_t cols, int lane, int32_t *patch) {                     \
+    switch (activation_kind(L.act)) { /* wave-uniform */                                                           \
+      case 0: NAME##_as<FM, FN, 0, FULL>(acc, L, row0, col0, rows, cols, lane, patch); break;                       \
+      case 1: NAME##_as<FM, FN, 1, FULL>(acc, L, row0, col0, rows, cols, lane, patch); break;                       \
+      default: NAME##_as<FM, FN, 2, FULL>(acc, L, row0, col0, rows, cols, lane, patch); break;                      \
+    }                                                                                                              \
+  }
+MIP_STORE_LINEAR(store_linear16, v4i)
+MIP_STORE_LINEAR(store_linear32, v16i)
+#undef MIP_STORE_LINEAR
+
+}  // namespace mip

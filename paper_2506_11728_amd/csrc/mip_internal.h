@@ -21,6 +21,17 @@ struct ConvGeom {
   int stride, pad;
 };
 
+enum Activation { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_GELU_TANH = 3, ACT_SILU = 4 };
+
+// What a linear layer does to the sums of its product (linear.h).
+struct LinearArgs {
+  void *C;
+  const void *R;  // null: no residual
+  int64_t ldc, ldr;
+  const float *row_scale, *col_scale, *bias;  // null: 1, 1, 0
+  int act, type;  // of C and R: RealType
+};
+
 struct Problem {
   int64_t m, n, k;
   const void *A;  // A(i,p) at A[i*a_sm + p*a_sk]
@@ -33,6 +44,7 @@ struct Problem {
   int accumulate;
   // 1: dequantised output (paper Section 7.3): C holds floats, float(sum) * scale
   // 2: requantised output: C holds int8 (ldc counts bytes), clip(rint(float(sum) * scale))
+  // 3: a linear layer (Problem::linear): C holds real numbers of a type of their own (ldc counts elements)
   int out_float;
   float scale;
   // batch > 1: that many independent problems of the same shape; problem z reads A + z*a_sb,
@@ -55,6 +67,7 @@ struct Problem {
   // tile kernels, the tiles whose waves split k and the row-segment kernel can; a_sm is then the nominal row length k)
   const ConvGeom *conv = nullptr;
   bool packed_weights = false;  // one operand is the library's packed weights
+  const LinearArgs *linear = nullptr;  // host memory; both operands signed, A row-major, C row-major, no batch
 };
 
 // Division by a number that the host knows: n / d = high word of n * inv, exact for every n <= most

@@ -130,7 +130,7 @@ static int use_packed(Problem *p, const void *Ap, const void *Bp) {
 int run_gemm(int a_unsigned, int b_unsigned, int out_float, float scale, int64_t m, int64_t n,
         int64_t k, const void *A, int64_t lda, int orderA, const void *B, int64_t ldb, int orderB,
         void *C, int64_t ldc, int orderC, int mode, void *workspace, size_t workspace_bytes,
-        void *stream, const Batch &batch, const int32_t *ksum) {
+        void *stream, const Batch &batch, const int32_t *ksum, const LinearArgs *linear) {
   Problem p;
   int rc = validate_and_normalise(a_unsigned, b_unsigned, m, n, k, A, lda, orderA, B, ldb, orderB,
                                   C, ldc, orderC, mode, workspace, workspace_bytes, &p);
@@ -139,6 +139,7 @@ int run_gemm(int a_unsigned, int b_unsigned, int out_float, float scale, int64_t
   p.ksum = (a_unsigned != 0) != (b_unsigned != 0) ? ksum : nullptr;
   p.packed_weights = ksum != nullptr;
   p.out_float = out_float;
+  p.linear = linear;
   p.scale = scale;
   p.batch = batch.count;
   // a column-major C has swapped the operand roles: the strides follow their operands
@@ -521,8 +522,10 @@ const char *mipgemm_strerror(int code) {
       "invalid argument 14 (workspace is null)",
       "invalid argument 15 (workspace_bytes too small)", "invalid argument 16 (stream)",
       "invalid argument 17 (scale is not finite)", "invalid argument 18", "invalid argument 19",
-      "invalid argument 20"};
-  if (code <= 0 && code >= -20) return args[-code];
+      "invalid argument 20", "invalid argument 21", "invalid argument 22", "invalid argument 23",
+      "invalid argument 24", "invalid argument 25", "invalid argument 26", "invalid argument 27",
+      "invalid argument 28", "invalid argument 29", "invalid argument 30"};
+  if (code <= 0 && code >= -30) return args[-code];
   if (code == MIPGEMM_ERR_STATIC_SCRATCH)
     return "the problem needs more scratch memory than the library's static buffer holds";
   if (code > 0) return hipGetErrorString(static_cast<hipError_t>(code));

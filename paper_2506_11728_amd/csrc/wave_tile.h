@@ -3,6 +3,7 @@
 #pragma once
 #include "dma_common.h"
 #include "epilogue16.h"
+#include "linear.h"
 
 namespace mip {
 
@@ -19,6 +20,9 @@ struct WaveTileParams {
   float scale;
   const int32_t *ksum;  // not null: the k sums of the signed operand (see Problem::ksum)
   int64_t a_sb, b_sb, c_sb;
+};
+struct WaveLinearParams : WaveTileParams {
+  LinearArgs linear;
 };
 struct WaveConvParams : WaveTileParams {
   ConvGeom conv;
@@ -72,14 +76,15 @@ struct WaveOperand {
 };
 
 // MT, NT: blocks of 16 rows and columns in a tile.  W: waves.
-// UNS: 0 both operands signed, 1 A unsigned, 2 B unsigned.
+// UNS: 0 both operands signed, 1 A unsigned, 2 B unsigned; LINEAR_OUT: both signed, the write-back of a linear layer.
 // A workgroup of W waves has one tile of 16 MT x 16 NT; wave w takes steps w, w + W, ... of 128 k through LDS
 // stages of its own, so that nothing but its own loads holds a wave up and the only barriers are those of the final
 // sum over LDS.  What bounds it is the rate at which a compute unit takes direct loads, 63 bytes a clock (more of
 // them per product the smaller the tile), and for a short k the latency of the first load and of the sum, some 3 us.
 // (512, 512, 2048) on 64 x 64 tiles that share each block among four waves took 6.5 us and takes 4.2 on these.
 template <int MT, int NT, int W, bool A_KC, bool B_KC, int UNS, Source SOURCE>
-__global__ __launch_bounds__(64 * W) void wave_tile_kernel(std::conditional_t<SOURCE == GATHERED, WaveConvParams, WaveTileParams> P) {
+__global__ __launch_bounds__(64 * W) void wave_tile_kernel(
+    std::conditional_t<SOURCE == GATHERED, WaveConvParams, std::conditional_t<UNS == LINEAR_OUT, WaveLinearParams, WaveTileParams>> P) {
   constexpr bool CONV = SOURCE == GATHERED, REGS = SOURCE == STAGED;
   static_assert(!CONV || (A_KC && B_KC && UNS == 1), "the lowered matrix is unsigned, it and the filters k-contiguous");
   using OA = WaveOperand<MT, A_KC>;
@@ -283,7 +288,7 @@ __global__ __launch_bounds__(64 * W) void wave_tile_kernel(std::conditional_t<SO
     for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        if (UNS != 0) acc[i][t] += 128 * accS[UNS == 1 ? t : i];
+        if (UNS == 1 || UNS == 2) acc[i][t] += 128 * accS[UNS == 1 ? t : i];
         *reinterpret_cast<v4i *>(mine + i * 16 * PITCH + 16 * t) = acc[i][t];
       }
   }
@@ -309,6 +314,19 @@ __global__ __launch_bounds__(64 * W) void wave_tile_kernel(std::conditional_t<SO
   for (int u = 0; u < PASSES; ++u) {
     const int at = tid + u * (64 * W), r = at / (BN / 4), c = 4 * (at % (BN / 4));
     if (r >= rows || c >= cols) continue;
+    if constexpr (UNS == LINEAR_OUT) {
+      const LinearColumns columns = linear_columns(P.linear, n0 + c, cols - c);
+      const float row_scale = P.linear.row_scale ? P.linear.row_scale[m0 + r] : 1.0f;
+      v4f residual = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (P.linear.R) residual = linear_residual(P.linear, m0 + r, n0 + c, cols - c);
+      const auto finish = [&](auto act) { linear_quad(P.linear, act, columns, m0 + r, n0 + c, cols - c, sum[u], row_scale, residual); };
+      switch (activation_kind(P.linear.act)) {  // wave-uniform
+        case 0: finish(Activate<0>::of(P.linear.act)); break;
+        case 1: finish(Activate<1>::of(P.linear.act)); break;
+        default: finish(Activate<2>::of(P.linear.act)); break;
+      }
+      continue;
+    }
     int32_t *dst = C + r * P.ldc + c;
     const bool whole = c + 3 < cols;
     v4i old = {0, 0, 0, 0};
@@ -317,7 +335,7 @@ __global__ __launch_bounds__(64 * W) void wave_tile_kernel(std::conditional_t<SO
       else
         for (int e = 0; e < cols - c; ++e) old[e] = dst[e];
     }
-    if (UNS != 0 && P.ksum) {
+    if ((UNS == 1 || UNS == 2) && P.ksum) {
       if (UNS == 1) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -394,13 +412,23 @@ hipError_t launch_wave_tile_for(const Problem &p, hipStream_t s) {
     }
   }
 #undef MIP_PICK
+  const void *args = &P;
+  WaveLinearParams PL;
+  if (p.linear) {
+    static_cast<WaveTileParams &>(PL) = P;
+    PL.linear = *p.linear;
+    args = &PL;
+    void (*linear)(WaveLinearParams) = b_kc ? wave_tile_kernel<MT, NT, W, true, true, LINEAR_OUT, SOURCE>
+                                            : wave_tile_kernel<MT, NT, W, true, false, LINEAR_OUT, SOURCE>;
+    kernel = reinterpret_cast<const void *>(linear);
+  }
   const size_t stages = (size_t)W * (MT + NT) * 2048, sums = (size_t)W * BM * (BN + 4) * 4;
   const size_t lds = stages > sums ? stages : sums;
   hipError_t e = allow_dynamic_lds(kernel, lds);
   if (e != hipSuccess) return e;
   const int64_t tiles = (int64_t)P.walk.tiles_m * P.walk.tiles_n;
   dim3 grid((unsigned)(((tiles + 7) / 8) * 8), 1, (unsigned)p.batch);
-  return launch_with(kernel, grid, 64 * W, lds, s, &P);
+  return launch_with(kernel, grid, 64 * W, lds, s, args);
 }
 
 }  // namespace mip

@@ -25,14 +25,22 @@ typedef int (*conv_fn)(q, q, q, q, q, q, q, q, q, p, p, p, int, p, size_t, p);
 typedef int (*conv_scaled_fn)(q, q, q, q, q, q, q, q, q, p, p, p, int, p, size_t, p, float);
 typedef int (*conv_sums_fn)(q, q, q, q, q, q, q, q, q, p, p, p, int, p, size_t, p, p);
 typedef int (*conv_scaled_sums_fn)(q, q, q, q, q, q, q, q, q, p, p, p, int, p, size_t, p, float, p);
+typedef int (*quantize_fn)(q, q, p, q, int, p, float, p, q, p, p);
+typedef int (*linear_fn)(q, q, q, p, q, p, p, q, int, p, p, int, p, q, p, q, int, p, size_t, p);
+typedef int (*rope_fn)(q, q, q, q, int, p, q, p, q, p, q, p, p, float, p, p, q, q, int, p, p, q, p, q, p, size_t, q, q, p, p);
+typedef int (*kv4_read_fn)(q, q, q, int, p, size_t, q, q, p, p, q, p, q, p);
+typedef int (*attention_fn)(q, q, q, q, int, p, q, q, p, q, p, q, p, size_t, q, q, p, q, float, p, q, p, size_t, p);
 
-enum { GEMM, GEMM_SCALED, BATCHED, PACKED, CONV, CONV_SCALED, CONV_SUMS, CONV_SCALED_SUMS, KINDS };
+enum { GEMM, GEMM_SCALED, BATCHED, PACKED, CONV, CONV_SCALED, CONV_SUMS, CONV_SCALED_SUMS,
+       QUANTIZE, LINEAR, ROPE, KV4_READ, ATTENTION, KINDS };
 
 /* q int64, i int, p pointer, z size, s stream, f float: the arguments of each kind in order */
 static const char *const kFormat[KINDS] = {
     "qqqpqipqipqiipzs",  "qqqpqipqipqiipzsf", "qqqpqiqpqiqpqiqqipzs", "qqqpqippqiipzs",
-    "qqqqqqqqqpppipzs",  "qqqqqqqqqpppipzsf", "qqqqqqqqqpppipzsp",    "qqqqqqqqqpppipzsfp"};
-#define MOST_ARGS 20
+    "qqqqqqqqqpppipzs",  "qqqqqqqqqpppipzsf", "qqqqqqqqqpppipzsp",    "qqqqqqqqqpppipzsfp",
+    "qqpqipfpqps", "qqqpqppqippipqpqipzs", "qqqqipqpqpqppfppqqippqpqpzqqps", "qqqipzqqppqpqs",
+    "qqqqipqqpqpqpzqqpqfpqpzs"};
+#define MOST_ARGS 30
 
 typedef union { q i; p ptr; float f; } value;
 
@@ -141,7 +149,26 @@ static PyObject *call(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
     case CONV: rc = ((conv_fn)e->fn)(CONV_ARGS); break;
     case CONV_SCALED: rc = ((conv_scaled_fn)e->fn)(CONV_ARGS, F(16)); break;
     case CONV_SUMS: rc = ((conv_sums_fn)e->fn)(CONV_ARGS, P(16)); break;
-    default: rc = ((conv_scaled_sums_fn)e->fn)(CONV_ARGS, F(16), P(17)); break;
+    case CONV_SCALED_SUMS: rc = ((conv_scaled_sums_fn)e->fn)(CONV_ARGS, F(16), P(17)); break;
+    case QUANTIZE:
+      rc = ((quantize_fn)e->fn)(Q(0), Q(1), P(2), Q(3), I(4), P(5), F(6), P(7), Q(8), P(9), P(10));
+      break;
+    case LINEAR:
+      rc = ((linear_fn)e->fn)(Q(0), Q(1), Q(2), P(3), Q(4), P(5), P(6), Q(7), I(8), P(9), P(10), I(11), P(12), Q(13),
+                              P(14), Q(15), I(16), P(17), Z(18), P(19));
+      break;
+    case ROPE:
+      rc = ((rope_fn)e->fn)(Q(0), Q(1), Q(2), Q(3), I(4), P(5), Q(6), P(7), Q(8), P(9), Q(10), P(11), P(12), F(13), P(14),
+                            P(15), Q(16), Q(17), I(18), P(19), P(20), Q(21), P(22), Q(23), P(24), Z(25), Q(26), Q(27),
+                            P(28), P(29));
+      break;
+    case KV4_READ:
+      rc = ((kv4_read_fn)e->fn)(Q(0), Q(1), Q(2), I(3), P(4), Z(5), Q(6), Q(7), P(8), P(9), Q(10), P(11), Q(12), P(13));
+      break;
+    default:
+      rc = ((attention_fn)e->fn)(Q(0), Q(1), Q(2), Q(3), I(4), P(5), Q(6), Q(7), P(8), Q(9), P(10), Q(11), P(12), Z(13),
+                                 Q(14), Q(15), P(16), Q(17), F(18), P(19), Q(20), P(21), Z(22), P(23));
+      break;
   }
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(rc);
