@@ -9,7 +9,8 @@
 // and both are exact.  Queries in bfloat16 are multiplied by a power of two that brings the row's largest
 // below 32768 and are exact as float16 wherever they are not 2^-24 times smaller than that; the power is
 // taken back in the scale of the scores.  What is rounded is p: to float16, eleven bits, less than the output's
-// own rounding.  Its sum is of the unrounded p.
+// own rounding in bfloat16.  Its sum, one more column of the product with the values, is of
+// the rounded p.
 //
 // Operand layout of the instruction: lane l gives row (column) l % 16, eight k from 8 (l / 16) on; the result has
 // column l % 16 and rows 4 (l / 16) .. + 3.  Any order of k will do that both operands share.
@@ -19,6 +20,8 @@
 //     tiles), and lane l takes for it, from the same eight tokens, the channels of its word l % 16, one of
 //     the word's eight nibbles to an instruction.
 #pragma once
+#include <type_traits>
+
 #include "kv4.h"
 #include "layer_internal.h"
 
@@ -111,15 +114,20 @@ __device__ __forceinline__ v2h as_halves(uint32_t w) { return __builtin_bit_cast
 // Steps and negated zero points of two pairs (one in either half of `pairs`).
 struct Kv4Scale {
   v2h s, z1024, z64;  // s, -(1024 + z), -(64 + z)
+  uint32_t e1024, e64;  // 1024 and 64 in both halves
   __device__ __forceinline__ explicit Kv4Scale(uint32_t pairs) {
     s = as_halves((pairs & 0x00ff00ffu) << 7);
     // z + 128 under the exponent of -1024, less the 128
     z1024 = as_halves(((pairs >> 8) & 0x00ff00ffu) ^ 0xe480e480u) + (_Float16)128.0f;
     z64 = z1024 + (_Float16)960.0f;
+    // (in registers the compiler knows nothing of: as literals, mask and exponent would take an instruction each)
+    e1024 = 0x64006400u;
+    e64 = 0x54005400u;
+    asm("" : "+v"(e1024), "+v"(e64));
   }
   // nibbles at bits 0 and 16, and at bits 4 and 20
-  __device__ __forceinline__ v2h low(uint32_t w) const { return (as_halves((w & 0x000f000fu) | 0x64006400u) + z1024) * s; }
-  __device__ __forceinline__ v2h high(uint32_t w) const { return (as_halves((w & 0x00f000f0u) | 0x54005400u) + z64) * s; }
+  __device__ __forceinline__ v2h low(uint32_t w) const { return (as_halves((w & 0x000f000fu) | e1024) + z1024) * s; }
+  __device__ __forceinline__ v2h high(uint32_t w) const { return (as_halves((w & 0x00f000f0u) | e64) + z64) * s; }
 };
 
 __device__ __forceinline__ v8h join(v2h a, v2h b, v2h c, v2h d) {
@@ -170,12 +178,30 @@ __device__ __forceinline__ Request request_of(const AttentionArgs &P, int r) {
   keys = keys < 0 ? 0 : (keys > P.max_kv ? P.max_kv : keys);
   return {a, (int)queries, (int)keys};
 }
-// The head's part of the page of a token, or null where the table names no page there.
-__device__ __forceinline__ const uint8_t *part_of(const AttentionArgs &P, int r, int head, int64_t token, int64_t block) {
-  const int64_t at = token >> P.log_page;
-  const int page = at < P.table_stride ? P.block_table[r * P.table_stride + at] : -1;
-  return page >= 0 && page < P.pages ? P.cache + ((int64_t)page * P.kv_heads + head) * block : nullptr;
-}
+// Where a request's keys and values of one head lie.
+struct Pages {
+  typedef const __attribute__((address_space(4))) int32_t *table_ptr;
+  table_ptr table;
+  const uint8_t *head;  // the head's part of page 0
+  int64_t bytes;        // from page to page
+  int last, pages, log_page;
+  __device__ __forceinline__ Pages(const AttentionArgs &P, int r, int of, int64_t block)
+      : table((table_ptr)(uintptr_t)(P.block_table + r * P.table_stride)), head(P.cache + of * block),
+        bytes(P.kv_heads * block), last((int)P.table_stride - 1), pages(P.pages), log_page(P.log_page) {}
+  // What the table says of a token's page: through the scalar cache (the table is not written while a kernel reads it),
+  // and asked for well ahead of the page's own loads, which would otherwise begin with a wait for it.
+  __device__ __forceinline__ int of(int token) const {
+    const int at = __builtin_amdgcn_readfirstlane(token) >> log_page;
+    return table[at < last ? at : last];
+  }
+  // whether it names a page there
+  __device__ __forceinline__ bool named(int page, int token) const {
+    return (unsigned)page < (unsigned)pages && (token >> log_page) <= last;
+  }
+  // the page, or one that is there to be read
+  __device__ __forceinline__ const uint8_t *part(int page, bool named) const { return head + (named ? page : 0) * bytes; }
+  __device__ __forceinline__ int within(int token) const { return token & ((1 << log_page) - 1); }
+};
 
 constexpr float LOWEST = -3.402823466e38f;
 // p is 2^(score - base) in float16, base the row's maximum less HEAD when it was last set: up to 2^LIMIT before
@@ -216,53 +242,67 @@ __device__ __forceinline__ float load_queries(const AttentionArgs &P, int64_t at
   return fmaxf(P.scale * 1.4426950408889634f * back, 1.2e-38f);
 }
 
-// p of 32 keys for a wave's sixteen rows (lane: row l % 16, tokens 4 (l / 16) .. + 3 of two tiles) from their scores,
-// as the operand of the output.  Only where a score has risen past LIMIT do the lanes of a row have to agree on a
-// new base (top), and are its sums rescaled.
-template <int CHANNELS>
-__device__ __forceinline__ v8h weights(const v4f (&score)[2], float scale, float &top, float &total, v4f (&out)[CHANNELS], int h) {
-  float x[8];
+// p of N times 32 keys for a wave's RT times sixteen rows (lane: row l % 16, tokens 4 (l / 16) .. + 3 of two tiles) from
+// their scores, as operands of the output.  Only where a score has risen past LIMIT do the lanes of a row have
+// to agree on a new base (top), and are its sums rescaled.  far: some base is so large that float32 holds no fractions of
+// it.
+template <int RT, int N, int SUMS>
+__device__ __forceinline__ void weights(const v4f (&score)[RT][N][2], const float (&scale)[RT], float (&top)[RT], bool &far,
+                                        v4f (&out)[RT][SUMS], int h, v8h (&p)[RT][N]) {
+  float x[RT][N][8];
   // A fused multiply-add keeps what the product's rounding would lose, but against a base that is a rounded product
   // itself the difference of two large numbers is no longer zero where they are equal: past 2^20 both are rounded.
-  auto exponents = [&] {
-    if (__any(fabsf(top) > 1048576.0f)) {
+  auto exponents = [&](auto rounded) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = __fsub_rn(__fmul_rn(score[e / 4][e % 4], scale), top);
-    } else {
+    for (int t = 0; t < RT; ++t)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = __builtin_fmaf(score[e / 4][e % 4], scale, -top);
-    }
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float s = score[t][n][e / 4][e % 4];
+          x[t][n][e] = decltype(rounded)::value ? __fsub_rn(__fmul_rn(s, scale[t]), top[t]) : __builtin_fmaf(s, scale[t], -top[t]);
+        }
   };
-  exponents();
+  if (far) exponents(std::true_type{});
+  else exponents(std::false_type{});
   float largest = LOWEST;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) largest = fmaxf(largest, x[e]);
+  for (int t = 0; t < RT; ++t)
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) largest = fmaxf(largest, x[t][n][e]);
   if (__any(largest > LIMIT)) {
-    largest = LOWEST;
+    far = false;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) largest = fmaxf(largest, __fmul_rn(score[e / 4][e % 4], scale));
-    largest = fmaxf(largest, __shfl_xor(largest, 16));
-    largest = fmaxf(largest, __shfl_xor(largest, 32));
-    const float moved = largest - HEAD > top ? largest - HEAD : top;
-    const float less = __builtin_amdgcn_exp2f(top - moved);
-    top = moved;
-    total *= less;
+    for (int t = 0; t < RT; ++t) {
+      largest = LOWEST;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float by = __shfl(less, 4 * h + e);
+      for (int n = 0; n < N; ++n)
 #pragma unroll
-      for (int j = 0; j < CHANNELS; ++j) out[j][e] *= by;
+        for (int e = 0; e < 8; ++e) largest = fmaxf(largest, __fmul_rn(score[t][n][e / 4][e % 4], scale[t]));
+      largest = fmaxf(largest, __shfl_xor(largest, 16));
+      largest = fmaxf(largest, __shfl_xor(largest, 32));
+      const float moved = largest - HEAD > top[t] ? largest - HEAD : top[t];
+      const float less = __builtin_amdgcn_exp2f(top[t] - moved);
+      top[t] = moved;
+      far |= __any(fabsf(moved) > 1048576.0f);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float by = __shfl(less, 4 * h + e);
+#pragma unroll
+        for (int j = 0; j < SUMS; ++j) out[t][j][e] *= by;
+      }
     }
-    exponents();
+    if (far) exponents(std::true_type{});
+    else exponents(std::false_type{});
   }
-  v8h p;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float y = __builtin_amdgcn_exp2f(x[e]);
-    total += y;
-    p[e] = (_Float16)y;
-  }
-  return p;
+  for (int t = 0; t < RT; ++t)
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[t][n][e] = (_Float16)__builtin_amdgcn_exp2f(x[t][n][e]);
 }
 
 }  // namespace mip

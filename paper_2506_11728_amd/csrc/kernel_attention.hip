@@ -18,7 +18,7 @@ template <int D>
 constexpr int PARTIAL = D + 4;
 
 template <int D, int TYPE, int RT>
-__global__ __launch_bounds__(64 * WAVES) void attention_rows_kernel(AttentionArgs P) {
+__global__ __launch_bounds__(64 * WAVES, D <= 128 && RT == 1 ? 4 : 1) void attention_rows_kernel(AttentionArgs P) {
   using S = Kv4Shape<D>;
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   auto sums = reinterpret_cast<float (*)[16][D + 4]>(smem);  // a wave's: sixteen rows
@@ -27,20 +27,24 @@ __global__ __launch_bounds__(64 * WAVES) void attention_rows_kernel(AttentionArg
   const int c = lane & 15, h = lane >> 4;
   const int range = blockIdx.x % P.ranges, of_all = P.first + blockIdx.x / P.ranges, r = blockIdx.z;
   const int head = of_all % P.kv_heads, tile = of_all / P.kv_heads;
+  // (the first pages are on their way with the request's numbers)
+  const int begin = range * P.span, mine = begin + wave * STEP;
+  const Pages pages(P, r, head, Kv4Layout(1 << P.log_page, D).block);
+  int page[2] = {pages.of(mine), pages.of(mine + 16)};
   const Request req = request_of(P, r);
   const int rows = req.queries * P.shared, row0 = tile * (16 * RT);
   if (row0 >= rows) return;
-  const int64_t block = Kv4Layout(1 << P.log_page, D).block;
   // keys that any row of the tile sees
   const int last_query = (row0 + 16 * RT < rows ? row0 + 16 * RT - 1 : rows - 1) / P.shared;
   const int seen = req.keys - req.queries + last_query + 1;
-  const int begin = range * P.span, end = P.partials ? (seen < begin + P.span ? seen : begin + P.span) : seen;
+  const int end = P.partials ? (seen < begin + P.span ? seen : begin + P.span) : seen;
   if (range > 0 && begin >= end) return;
 
   v8h q[RT][S::KEY_STEPS];
-  float scale[RT], top[RT], total[RT];
+  float scale[RT], top[RT];
+  bool far = true;  // (the first base is)
   int sees[RT];  // keys that the row sees
-  v4f out[RT][S::CHANNELS];
+  v4f out[RT][S::CHANNELS + 1];  // the last: sums of p
   int fewest = 0x7fffffff;
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
@@ -54,14 +58,14 @@ __global__ __launch_bounds__(64 * WAVES) void attention_rows_kernel(AttentionArg
     const int least = row0 + 16 * t + 15 < rows ? req.keys - req.queries + first_query + 1 : 0;
     fewest = least < fewest ? least : fewest;
     top[t] = LOWEST;
-    total[t] = 0.0f;
 #pragma unroll
-    for (int j = 0; j < S::CHANNELS; ++j) out[t][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int j = 0; j <= S::CHANNELS; ++j) out[t][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
+  const _Float16 one = (_Float16)1.0f;
+  const v8h ones = {one, one, one, one, one, one, one, one};
   const Kv4Reader<D> reader(P.log_page, lane);
   const int steps = end > begin ? (end - begin + STEP - 1) / STEP : 0;
-  const int mask = (1 << P.log_page) - 1;
   Kv4Tile<D> next[2];
   bool named[2];  // the table names a page for the tile
   auto fetch = [&](int step) {
@@ -69,9 +73,9 @@ __global__ __launch_bounds__(64 * WAVES) void attention_rows_kernel(AttentionArg
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int first = token + 16 * u;
-      const uint8_t *part = first < end ? part_of(P, r, head, first, block) : nullptr;
-      named[u] = part != nullptr;
-      reader.load(named[u] ? part : P.cache, named[u] ? first & mask : 0, next[u]);
+      named[u] = pages.named(page[u], first);
+      reader.load(pages.part(page[u], named[u]), pages.within(first), next[u]);
+      page[u] = pages.of(first + WAVES * STEP);  // for the step after
     }
   };
   if (wave < steps) fetch(wave);
@@ -81,11 +85,11 @@ __global__ __launch_bounds__(64 * WAVES) void attention_rows_kernel(AttentionArg
     if (step + WAVES < steps) fetch(step + WAVES);
     const int token = begin + step * STEP;
 
-    v4f score[RT][2];
+    v4f score[RT][1][2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
 #pragma unroll
-      for (int t = 0; t < RT; ++t) score[t][u] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int t = 0; t < RT; ++t) score[t][0][u] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int n = 0; n < S::UNITS; ++n) {
         const Kv4Scale g(now[u].key_pair[n] * 0x00010001u);
@@ -93,7 +97,7 @@ __global__ __launch_bounds__(64 * WAVES) void attention_rows_kernel(AttentionArg
         for (int w = 0; w < S::WORDS; ++w) {
           const v8h k = key_operand(now[u].key[n][w], g);
 #pragma unroll
-          for (int t = 0; t < RT; ++t) score[t][u] = multiply(k, q[t][n * S::WORDS + w], score[t][u]);
+          for (int t = 0; t < RT; ++t) score[t][0][u] = multiply(k, q[t][n * S::WORDS + w], score[t][0][u]);
         }
       }
     }
@@ -101,26 +105,26 @@ __global__ __launch_bounds__(64 * WAVES) void attention_rows_kernel(AttentionArg
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int at = token + 16 * u + 4 * h + e;
+        for (int t = 0; t < RT; ++t) {
+          const int room = (known[u] ? sees[t] : 0) - (token + 16 * u + 4 * h);
 #pragma unroll
-          for (int t = 0; t < RT; ++t)
-            if (at >= sees[t] || !known[u]) score[t][u][e] = -__builtin_inff();
+          for (int e = 0; e < 4; ++e) score[t][0][u][e] = e < room ? score[t][0][u][e] : -__builtin_inff();
         }
       // what lies behind the last key, and in pages that are none, is no number: a step of zero makes it zero
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < 2; ++u) {
+        const int exist = known[u] ? end - (token + 16 * u + 4 * h) : 0;
 #pragma unroll
-        for (int n = 0; n < S::UNITS; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (token + 16 * u + 4 * h + e >= end || !known[u])
-              now[u].value_pair[n][e / 2] &= e & 1 ? 0x0000ffff : (int)0xffff0000;
+        for (int n = 0; n < S::UNITS; ++n) {
+          if (exist < 4) now[u].value_pair[n][1] &= exist < 3 ? 0 : 0x0000ffff;
+          if (exist < 2) now[u].value_pair[n][0] &= exist < 1 ? 0 : 0x0000ffff;
+        }
+      }
     }
-    v8h p[RT];
+    v8h p[RT][1];
+    weights(score, scale, top, far, out, h, p);
 #pragma unroll
-    for (int t = 0; t < RT; ++t)
-      p[t] = weights(score[t], scale[t], top[t], total[t], out[t], h);
+    for (int t = 0; t < RT; ++t) out[t][S::CHANNELS] = multiply(p[t][0], ones, out[t][S::CHANNELS]);
 #pragma unroll
     for (int n = 0; n < S::UNITS; ++n) {
       const Kv4Values<D> values(now[0].value[n], now[1].value[n], now[0].value_pair[n], now[1].value_pair[n], lane);
@@ -131,8 +135,8 @@ __global__ __launch_bounds__(64 * WAVES) void attention_rows_kernel(AttentionArg
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
           v4f &a = out[t][n * S::NIBBLES + 2 * k], &b = out[t][n * S::NIBBLES + 2 * k + 1];
-          a = multiply(p[t], even, a);
-          b = multiply(p[t], odd, b);
+          a = multiply(p[t][0], even, a);
+          b = multiply(p[t][0], odd, b);
         }
       }
     }
@@ -142,19 +146,15 @@ __global__ __launch_bounds__(64 * WAVES) void attention_rows_kernel(AttentionArg
   const int row_in = tid >> 4, part = tid & 15;
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
-    float all = total[t];
-    all += __shfl_xor(all, 16);
-    all += __shfl_xor(all, 32);
     if (t > 0) __syncthreads();
-    if (h == 0) {
-      tops[wave][c] = top[t];
-      totals[wave][c] = all;
-    }
+    if (h == 0) tops[wave][c] = top[t];
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
+    for (int e = 0; e < 4; ++e) {
+      if (c == 0) totals[wave][4 * h + e] = out[t][S::CHANNELS][e];
 #pragma unroll
       for (int j = 0; j < S::CHANNELS; ++j)
         sums[wave][4 * h + e][S::value_channel(j / S::NIBBLES, j % S::NIBBLES, c)] = out[t][j][e];
+    }
     __syncthreads();
     const int row = row0 + 16 * t + row_in;
     float m = tops[0][row_in], l = 0.0f, o[D / 16];
@@ -188,14 +188,18 @@ __global__ __launch_bounds__(64 * WAVES) void attention_rows_kernel(AttentionArg
   }
 }
 
-// The kernel for many rows.  A workgroup of W waves takes 16 RT W rows of one request and key head; tiles of 64 keys
+// The kernel for many rows.  A workgroup of eight waves takes 128 RT rows of one request and key head; tiles of 64 keys
 // are brought from codes to float16 once for all of them, each wave its share, and lie in LDS as the operands the
-// instructions take, 1 KB each, so that every read is sixteen bytes a lane in a row.  Two stages: the codes of the
-// tile after next are on their way while the next one's are written and the present one is multiplied.
-template <int D, int TYPE, int RT, int W>
-__global__ __launch_bounds__(64 * W, W / 4) void attention_tiles_kernel(AttentionArgs P) {
+// instructions take, 1 KB each, so that every read is sixteen bytes a lane in a row.
+//
+// A SIMD has two waves, one of either half of the workgroup, and the halves run half a tile apart, held there by a
+// barrier after every half: while one wave keeps the matrix unit busy (output of a tile, scores of the next), the other
+// has the vector unit to itself (weights of a tile, its share of the codes to come).  Side by side they took the
+// two units in turns: 2048 queries of 32 heads over 8192 keys 335 us, NOW us apart.
+template <int D, int TYPE, int RT>
+__global__ __launch_bounds__(512, 2) void attention_tiles_kernel(AttentionArgs P) {
   using S = Kv4Shape<D>;
-  constexpr int TILE = 64, KEYS = 4 * S::KEY_STEPS, VALUES = 2 * S::CHANNELS, STAGE = (KEYS + VALUES) * 1024;
+  constexpr int W = 8, TILE = 64, KEYS = 4 * S::KEY_STEPS, VALUES = 2 * S::CHANNELS;  // operands of a tile
   constexpr int KEY_PARTS = W / 4, KEY_EACH = S::KEY_STEPS / KEY_PARTS;  // a wave's share of a tile of sixteen keys
   constexpr int PAIRS = S::CHANNELS / 2, VALUE_PARTS = W / 2 < PAIRS ? W / 2 : PAIRS, VALUE_EACH = PAIRS / VALUE_PARTS;
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
@@ -206,21 +210,26 @@ __global__ __launch_bounds__(64 * W, W / 4) void attention_tiles_kernel(Attentio
   // the last rows of a prompt see the most keys: they begin first
   const int of_all = P.first + (int)(gridDim.x / P.ranges) - 1 - (int)(blockIdx.x / P.ranges);
   const int head = of_all % P.kv_heads, row0 = of_all / P.kv_heads * (16 * RT * W);
+  const int key_tile = wave & 3, key_part = wave >> 2, step = wave & 1, value_part = wave >> 1;
+  const int begin = range * P.span;
+  const Pages pages(P, r, head, Kv4Layout(1 << P.log_page, D).block);
+  int key_page = pages.of(begin + 16 * key_tile);
+  int value_page[2] = {pages.of(begin + 32 * step), pages.of(begin + 32 * step + 16)};
   const Request req = request_of(P, r);
   const int rows = req.queries * P.shared;
   if (row0 >= rows) return;
-  const int64_t block = Kv4Layout(1 << P.log_page, D).block;
   const int before = req.keys - req.queries + 1;  // keys that the first query sees
   auto sees_of = [&](int row) { return before + row / P.shared; };
   const int seen = sees_of(row0 + 16 * RT * W < rows ? row0 + 16 * RT * W - 1 : rows - 1);
-  const int begin = range * P.span, end = P.partials && begin + P.span < seen ? begin + P.span : seen;
+  const int end = P.partials && begin + P.span < seen ? begin + P.span : seen;
   if (range > 0 && begin >= end) return;
 
   const int wave_row = row0 + wave * (16 * RT);
   v8h q[RT][S::KEY_STEPS];
-  float scale[RT], top[RT], total[RT];
+  float scale[RT], top[RT];
+  bool far = true;  // (the first base is)
   int sees[RT];
-  v4f out[RT][S::CHANNELS];
+  v4f out[RT][S::CHANNELS + 1];  // the last: sums of p
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     const int row = wave_row + 16 * t + c;
@@ -230,134 +239,187 @@ __global__ __launch_bounds__(64 * W, W / 4) void attention_tiles_kernel(Attentio
     scale[t] = load_queries<D, TYPE>(P, at, here, h, q[t]);
     sees[t] = here ? before + query : 0;
     top[t] = LOWEST;
-    total[t] = 0.0f;
 #pragma unroll
-    for (int j = 0; j < S::CHANNELS; ++j) out[t][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int j = 0; j <= S::CHANNELS; ++j) out[t][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
   }
   // the fewest and the most keys that a row of the wave sees
   const int wave_end = wave_row + 16 * RT < rows ? wave_row + 16 * RT : rows;
   const int fewest = wave_row + 16 * RT <= rows ? sees_of(wave_row) : 0, most = wave_row < rows ? sees_of(wave_end - 1) : 0;
 
+  const _Float16 one = (_Float16)1.0f;
+  const v8h ones = {one, one, one, one, one, one, one, one};
   const Kv4Reader<D> reader(P.log_page, lane);
-  const int mask = (1 << P.log_page) - 1;
   const int tiles = end > begin ? (end - begin + TILE - 1) / TILE : 0;
   // a wave's share: keys of tile `wave % 4`, values of the tiles 2 (wave % 2) and the one after
-  const int key_tile = wave & 3, key_part = wave >> 2, step = wave & 1, value_part = wave >> 1;
   uint32_t key[KEY_EACH], key_pair;
   v4u value[2][S::UNITS];
   v2i value_pair[2][S::UNITS];
-  bool key_named, value_named[2];
-  int taken = 0;  // the token that the codes in registers begin with
-  auto fetch = [&](int tile) {
-    taken = begin + tile * TILE;
-    {
-      const int first = taken + 16 * key_tile;
-      const uint8_t *part = first < end ? part_of(P, r, head, first, block) : nullptr;
-      key_named = part != nullptr;
-      reader.template load_keys<KEY_EACH>(key_named ? part : P.cache, key_named ? first & mask : 0, key_part * KEY_EACH, key, key_pair);
-    }
+  bool key_named;
+  // (past the last tile, the last again: what it becomes is not used)
+  auto first_of = [&](int tile) { return begin + (tile < tiles ? tile : tiles - 1) * TILE; };
+  auto fetch_keys = [&](int tile) {
+    const int first = first_of(tile) + 16 * key_tile;
+    key_named = pages.named(key_page, first);
+    reader.template load_keys<KEY_EACH>(pages.part(key_page, key_named), pages.within(first), key_part * KEY_EACH, key, key_pair);
+  };
+  // the pages of the tiles that come after those: asked for at the start of a half, since its end waits for them
+  int next_key_page = 0, next_value_page[2] = {0, 0};
+  auto ask = [&](int of_keys, int of_values) {
+    next_key_page = pages.of(first_of(of_keys) + 16 * key_tile);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) next_value_page[i] = pages.of(first_of(of_values) + 32 * step + 16 * i);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto told = [&] {
+    key_page = next_key_page;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) value_page[i] = next_value_page[i];
+  };
+  auto fetch_values = [&](int tile) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int first = taken + 32 * step + 16 * i;
-      const uint8_t *part = first < end ? part_of(P, r, head, first, block) : nullptr;
-      value_named[i] = part != nullptr;
-      reader.load_values(value_named[i] ? part : P.cache, value_named[i] ? first & mask : 0, value[i], value_pair[i]);
+      const int first = first_of(tile) + 32 * step + 16 * i;
+      const bool exists = pages.named(value_page[i], first);
+      reader.load_values(pages.part(value_page[i], exists), pages.within(first), value[i], value_pair[i]);
+      // what lies behind the last key, and in pages that are none, is no number: a step of zero makes it zero
+      const int exist = exists ? end - first - 4 * h : 0;
+#pragma unroll
+      for (int n = 0; n < S::UNITS; ++n) {
+        if (exist < 4) value_pair[i][n][1] &= exist < 3 ? 0 : 0x0000ffff;
+        if (exist < 2) value_pair[i][n][0] &= exist < 1 ? 0 : 0x0000ffff;
+      }
     }
   };
-  auto unpack = [&](int stage) {
-    uint8_t *to = smem + stage * STAGE + 16 * lane;
+  auto unpack_keys = [&](int stage) {
+    uint8_t *to = smem + stage * (KEYS * 1024) + 16 * lane;
     const Kv4Scale g(key_pair * 0x00010001u);
 #pragma unroll
     for (int i = 0; i < KEY_EACH; ++i)
       *reinterpret_cast<v8h *>(to + (key_tile * S::KEY_STEPS + key_part * KEY_EACH + i) * 1024) = key_operand(key[i], g);
-    if (key_part == 0 && lane == 0) named[stage][key_tile] = key_named;
+    if (key_part == 0) named[stage][key_tile] = key_named;
+  };
+  auto unpack_values = [&](int stage) {
     if (value_part >= VALUE_PARTS) return;
-    // what lies behind the last key, and in pages that are none, is no number: a step of zero makes it zero
-    if (taken + TILE > end || !value_named[0] || !value_named[1]) {
+    uint8_t *to = smem + (2 * KEYS + stage * VALUES + step * S::CHANNELS) * 1024 + 16 * lane;
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int n = 0; n < S::UNITS; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (taken + 32 * step + 16 * i + 4 * h + e >= end || !value_named[i])
-              value_pair[i][n][e / 2] &= e & 1 ? 0x0000ffff : (int)0xffff0000;
+    for (int i = 0; i < VALUE_EACH; ++i) {
+      const int pair = value_part * VALUE_EACH + i, n = VALUE_EACH * VALUE_PARTS == PAIRS && S::UNITS == 1 ? 0 : pair / (S::NIBBLES / 2);
+      v8h even, odd;
+      // (a unit's registers by a wave-uniform choice)
+      const bool second = S::UNITS == 2 && n == 1;
+      const Kv4Values<D> values(second ? value[0][S::UNITS - 1] : value[0][0], second ? value[1][S::UNITS - 1] : value[1][0],
+                                second ? value_pair[0][S::UNITS - 1] : value_pair[0][0],
+                                second ? value_pair[1][S::UNITS - 1] : value_pair[1][0], lane);
+      values.pair(pair % (S::NIBBLES / 2), even, odd);
+      *reinterpret_cast<v8h *>(to + (2 * pair) * 1024) = even;
+      *reinterpret_cast<v8h *>(to + (2 * pair + 1) * 1024) = odd;
     }
-    to += (KEYS + step * S::CHANNELS) * 1024;
+  };
+  v4f score[RT][2][2];
+  v8h p[RT][2];
+  // Output of the values in one stage (VALUES_TOO) and scores of the keys in another, as one run of operands: each is read
+  // LOOK before it is used, in this order and no other, since left to itself the compiler reads two and waits for
+  // them.
+  auto multiply_tiles = [&](auto values_tag, auto keys_tag, int value_stage, int key_stage) {
+    constexpr int V = decltype(values_tag)::value ? VALUES : 0, N = V + (decltype(keys_tag)::value ? KEYS : 0), LOOK = 4;
+    const uint8_t *values = smem + (2 * KEYS + value_stage * VALUES) * 1024 + 16 * lane;
+    const uint8_t *keys = smem + key_stage * (KEYS * 1024) + 16 * lane;
+    auto read = [&](int i) { return *reinterpret_cast<const v8h *>(i < V ? values + i * 1024 : keys + (i - V) * 1024); };
+    v8h ring[LOOK];
 #pragma unroll
-    for (int n = 0; n < S::UNITS; ++n) {
-      const Kv4Values<D> values(value[0][n], value[1][n], value_pair[0][n], value_pair[1][n], lane);
+    for (int i = 0; i < LOOK; ++i) ring[i] = read(i);
 #pragma unroll
-      for (int k = 0; k < S::NIBBLES / 2; ++k) {
-        const int pair = n * (S::NIBBLES / 2) + k;
-        if (pair / VALUE_EACH != value_part) continue;
-        v8h even, odd;
-        values.pair(k, even, odd);
-        *reinterpret_cast<v8h *>(to + (2 * pair) * 1024) = even;
-        *reinterpret_cast<v8h *>(to + (2 * pair + 1) * 1024) = odd;
+    for (int i = 0; i < N; ++i) {
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        if (i < V) {
+          const int half = i / S::CHANNELS, j = i % S::CHANNELS;
+          if (j == 0) out[t][S::CHANNELS] = multiply(p[t][half], ones, out[t][S::CHANNELS]);
+          out[t][j] = multiply(p[t][half], ring[i % LOOK], out[t][j]);
+        } else {
+          const int u = (i - V) / S::KEY_STEPS, w = (i - V) % S::KEY_STEPS;
+          if (w == 0) score[t][u / 2][u % 2] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+          score[t][u / 2][u % 2] = multiply(ring[i % LOOK], q[t][w], score[t][u / 2][u % 2]);
+        }
       }
+      if (i + LOOK < N) ring[i % LOOK] = read(i + LOOK);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  auto mask_scores = [&](int tile) {
+    const int token = begin + tile * TILE;
+    const v4i all_named = *reinterpret_cast<const v4i *>(named[tile & 1]);
+    if (token + TILE > fewest || !__builtin_amdgcn_readfirstlane(all_named[0] & all_named[1] & all_named[2] & all_named[3])) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          const int room = (all_named[u] ? sees[t] : 0) - (token + 16 * u + 4 * h);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) score[t][u / 2][u % 2][e] = e < room ? score[t][u / 2][u % 2][e] : -__builtin_inff();
+        }
     }
   };
 
+  // (not __syncthreads: loads from memory stay in flight across it)
+  auto half_done = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+
+  // Half h of the first four waves is the output of tile h / 2 - 1 and the scores of tile h / 2 where h is even, the weights of
+  // tile h / 2 where it is odd; the other four are one half behind.  With two stages each, the keys of a tile and
+  // the values of the tile before are read in the halves 2 i and 2 i + 1.  The first four write the values of tile i
+  // and the keys of i + 1 in half 2 i + 1, the others the same in half 2 i, ahead of it by a tile: after the last
+  // reads of what they overwrite, before the first of theirs.
+  const int ahead = wave >> 2;
   if (tiles > 0) {
-    fetch(0);
-    unpack(0);
-  }
-  if (tiles > 1) fetch(1);
-  __syncthreads();
-  for (int tile = 0; tile < tiles; ++tile) {
-    const int stage = tile & 1, token = begin + tile * TILE;
-    if (tile + 1 < tiles) unpack(stage ^ 1);
-    if (tile + 2 < tiles) fetch(tile + 2);
-    if (token < most) {
-      const uint8_t *from = smem + stage * STAGE + 16 * lane;
-      v4f score[RT][2][2];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-#pragma unroll
-        for (int t = 0; t < RT; ++t) score[t][u / 2][u % 2] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int i = 0; i < S::KEY_STEPS; ++i) {
-          const v8h k = *reinterpret_cast<const v8h *>(from + (u * S::KEY_STEPS + i) * 1024);
-#pragma unroll
-          for (int t = 0; t < RT; ++t) score[t][u / 2][u % 2] = multiply(k, q[t][i], score[t][u / 2][u % 2]);
-        }
-      }
-      const v4i all_named = *reinterpret_cast<const v4i *>(named[stage]);
-      if (token + TILE > fewest || !__builtin_amdgcn_readfirstlane(all_named[0] & all_named[1] & all_named[2] & all_named[3])) {
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int t = 0; t < RT; ++t)
-              if (token + 16 * u + 4 * h + e >= sees[t] || !all_named[u]) score[t][u / 2][u % 2][e] = -__builtin_inff();
-      }
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        v8h p[RT];
-#pragma unroll
-        for (int t = 0; t < RT; ++t) p[t] = weights(score[t][half], scale[t], top[t], total[t], out[t], h);
-#pragma unroll
-        for (int j = 0; j < S::CHANNELS; ++j) {
-          const v8h v = *reinterpret_cast<const v8h *>(from + (KEYS + half * S::CHANNELS + j) * 1024);
-#pragma unroll
-          for (int t = 0; t < RT; ++t) out[t][j] = multiply(p[t], v, out[t][j]);
-        }
-      }
+    ask(1, 1);
+    fetch_keys(0);
+    unpack_keys(0);
+    fetch_values(0);
+    told();
+    fetch_keys(1);
+    ask(2, 1);
+    half_done();
+    told();
+    if (ahead) {
+      ask(3, 2);
+      unpack_values(0);
+      unpack_keys(1);
+      fetch_values(1);
+      fetch_keys(2);
+      half_done();
+      told();
     }
-    __syncthreads();
+    for (int tile = 0; tile < tiles; ++tile) {
+      const bool sees_any = begin + tile * TILE < most;
+      if (sees_any) {
+        if (tile > 0) multiply_tiles(std::true_type{}, std::true_type{}, (tile - 1) & 1, tile & 1);
+        else multiply_tiles(std::false_type{}, std::true_type{}, 0, 0);
+      }
+      half_done();
+      ask(tile + ahead + 3, tile + ahead + 2);
+      if (sees_any) {
+        mask_scores(tile);
+        weights(score, scale, top, far, out, h, p);
+      }
+      unpack_values((tile + ahead) & 1);
+      unpack_keys((tile + ahead + 1) & 1);
+      fetch_values(tile + ahead + 1);
+      fetch_keys(tile + ahead + 2);
+      told();
+      half_done();
+      // (the rows of a wave that see nothing of the next tile end here)
+      if (sees_any && (tile + 1 == tiles || begin + (tile + 1) * TILE >= most)) 
+        multiply_tiles(std::true_type{}, std::false_type{}, tile & 1, 0);
+    }
+    if (!ahead) half_done();
   }
 
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
-    float all = total[t];
-    all += __shfl_xor(all, 16);
-    all += __shfl_xor(all, 32);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int row = wave_row + 16 * t + 4 * h + e;
-      const float l = __shfl(all, 4 * h + e), m = __shfl(top[t], 4 * h + e);
+      const float l = out[t][S::CHANNELS][e], m = __shfl(top[t], 4 * h + e);
       if (row >= rows) continue;
       const int query = row / P.shared, within = row - query * P.shared;
       const float by = P.partials ? 1.0f : (l != 0.0f ? 1.0f / l : 0.0f);  // (a row that sees nothing: zeros)
@@ -448,7 +510,7 @@ Cut cut_call(int64_t requests, int64_t kv_heads, int64_t shared, int head_dim, i
   cut.rows = rows <= 16 ? 16 : (rows <= 32 ? 32 : (rows <= 128 || head_dim == 256 ? 128 : 256));
   const int64_t groups = requests * kv_heads * ((rows + cut.rows - 1) / cut.rows);
   const int64_t round = cut.tiles ? 64 : WAVES * STEP;  // keys between two barriers, or of all waves' steps
-  int64_t want = ((cut.tiles ? 1 : 2) * compute_units() + groups - 1) / groups;
+  int64_t want = ((cut.tiles ? 1 : 6) * compute_units() + groups - 1) / groups;
   const int64_t least = cut.tiles ? 8 : 4;  // rounds to a range
   const int64_t most = (max_kv + least * round - 1) / (least * round);
   if (want > most) want = most;
@@ -470,12 +532,11 @@ hipError_t launch_for(const AttentionArgs &P, const Cut &cut, int requests, hipS
   unsigned threads = 256;
   size_t lds = (size_t)WAVES * 16 * (D + 4) * 4;
   if (cut.tiles) {
-    const bool eight = cut.rows == 128 * RT;
-    kernel = attention_tiles_kernel<D, TYPE, RT, 8>;
+    kernel = attention_tiles_kernel<D, TYPE, 1>;
     if constexpr (RT == 2) {
-      if (!eight) kernel = attention_tiles_kernel<D, TYPE, RT, 4>;
+      if (cut.rows == 256) kernel = attention_tiles_kernel<D, TYPE, RT>;
     }
-    threads = eight ? 512 : 256;
+    threads = 512;
     lds = (size_t)(D / 4) * 2048;
   } else {
     kernel = cut.rows == 16 ? attention_rows_kernel<D, TYPE, 1> : attention_rows_kernel<D, TYPE, 2>;

@@ -6,7 +6,8 @@
 //
 // Bound by memory: x is read once, a byte an element written.  A row stays in the registers of its workgroup
 // between the reduction and the rounding where it fits (16384 numbers); longer rows are read a second time,
-// through the cache.  A wave to a row up to 1024 columns, four waves up to 16384, sixteen beyond.
+// through the cache.  A wave to a row up to 1024 columns, four waves up to 4096; up to 16384 sixteen waves
+// where there is a workgroup of them at a time for every row (48 rows of 11008: LATER us against 6.8 with four), else four.
 #include "layer_internal.h"
 #include "real.h"
 
@@ -37,21 +38,22 @@ template <typename T>
 __device__ __forceinline__ void load_oct(const QuantizeParams &P, int64_t row, int64_t j, float (&x)[8]) {
   constexpr int TYPE = real_of<T>::type;
   if (j + 8 <= P.cols) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const v4f v = load_real4(P.X, row * P.ldx + j + 4 * h, TYPE);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[4 * h + e] = v[e];
-    }
+    load_real8<TYPE>(P.X, row * P.ldx + j, x);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = j + e < P.cols ? load_real(P.X, row * P.ldx + j + e, TYPE) : 0.0f;
   }
 }
 __device__ __forceinline__ void times_weight(const QuantizeParams &P, int64_t j, float (&x)[8]) {
+  float w[8];
+  if (j + 8 <= P.cols) {
+    load_real8<REAL_F32>(P.weight, j, w);
+  } else {
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
-    if (j + e < P.cols) x[e] = __fmul_rn(x[e], P.weight[j + e]);
+    for (int e = 0; e < 8; ++e) w[e] = j + e < P.cols ? P.weight[j + e] : 0.0f;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = __fmul_rn(x[e], w[e]);
 }
 
 // The quotient num / a for |num| <= 127 a, correctly rounded: the reciprocal r of a is, and one step of
@@ -159,8 +161,9 @@ hipError_t launch_for(const QuantizeParams &P, hipStream_t s) {
   int64_t rows = 1;
   if (P.cols <= 1024) { kernel = quantize_kernel<T, 1, 4, 2>; rows = 4; }
   else if (P.cols <= 4096) kernel = quantize_kernel<T, 4, 1, 2>;
-  else if (P.cols <= 16384) kernel = quantize_kernel<T, 4, 1, 8>;
-  else { kernel = quantize_kernel<T, 16, 1, 0>; threads = 1024; }
+  else if (P.cols > 16384) { kernel = quantize_kernel<T, 16, 1, 0>; threads = 1024; }
+  else if (P.rows <= 2 * compute_units()) { kernel = quantize_kernel<T, 16, 1, 2>; threads = 1024; }
+  else kernel = quantize_kernel<T, 4, 1, 8>;
   const dim3 grid((unsigned)((P.rows + rows - 1) / rows));
   return launch_with(reinterpret_cast<const void *>(kernel), grid, threads, 0, s, &P);
 }

@@ -32,44 +32,69 @@ struct Kv4Layout {
 constexpr double KV4_TOP = 57344.0;
 
 // num / s, correctly rounded (r is 1 / s, correctly rounded; Markstein's theorem).
-__device__ __forceinline__ double kv4_quotient(double num, double s, double r) {
-  const double q = num * r;
-  return __builtin_fma(__builtin_fma(-q, s, num), r, q);
+template <typename F>
+__device__ __forceinline__ F kv4_quotient(F num, F s, F r) {
+  const F q = num * r;
+  if constexpr (sizeof(F) == 8) return __builtin_fma(__builtin_fma(-q, s, num), r, q);
+  else return __builtin_fmaf(__builtin_fmaf(-q, s, num), r, q);
 }
 
 // A lane's eight channels of a group that four neighbouring lanes hold: the word of codes, and the pair of the
-// group (in every lane).  All four lanes call it.
-__device__ __forceinline__ uint32_t kv4_encode(const double (&x)[8], uint32_t *pair) {
-  double lo = 0, hi = 0, v[8];
+// group (in every lane).  All four lanes call it.  In float32, `unsure` is set where an error of `error` in a channel, and of
+// the roundings here, could move a code or the step: there the caller does it again in float64.  (Without an error,
+// numbers of 16 bits leave nothing to be unsure of but the step: their quotients by four significant bits are
+// further from the middle between two codes than a rounding, or on it.)
+template <typename F>
+__device__ __forceinline__ uint32_t kv4_encode(const F (&x)[8], F error, uint32_t *pair, bool *unsure) {
+  constexpr bool WIDE = sizeof(F) == 8;
+  F lo = 0, hi = 0, v[8];
   int bad = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     bad |= !(x[e] - x[e] == 0);
-    v[e] = x[e] > KV4_TOP ? KV4_TOP : (x[e] < -KV4_TOP ? -KV4_TOP : x[e]);
+    v[e] = x[e] > (F)KV4_TOP ? (F)KV4_TOP : (x[e] < -(F)KV4_TOP ? -(F)KV4_TOP : x[e]);
     lo = e == 0 || v[e] < lo ? v[e] : lo;
     hi = e == 0 || v[e] > hi ? v[e] : hi;
   }
 #pragma unroll
   for (int d = 1; d < 4; d *= 2) {
-    const double l = __shfl_xor(lo, d), h = __shfl_xor(hi, d);
+    const F l = __shfl_xor(lo, d), h = __shfl_xor(hi, d);
     lo = l < lo ? l : lo;
     hi = h > hi ? h : hi;
     bad |= __shfl_xor(bad, d);
   }
+  *unsure = false;
   if (bad) {
     *pair = 0xff;
     return 0;
   }
-  const double range = (hi - lo) / 15, size = (hi > -lo ? hi : -lo) / 112;
-  const double step = range > size ? range : size;
-  const double s = step < 0x1p-14 ? __builtin_ceil(step * 0x1p17) * 0x1p-17
-                                  : __longlong_as_double((__double_as_longlong(step) + ((1LL << 49) - 1)) & ~((1LL << 49) - 1));
-  const double over = s > 0 ? s : 1.0, r = 1.0 / over;
-  const double z = -__builtin_rint(kv4_quotient(lo, over, r));
+  const F most = hi > -lo ? hi : -lo;
+  const F range = WIDE ? (hi - lo) / 15 : (hi - lo) * (F)(1.0 / 15), size = WIDE ? most / 112 : most * (F)(1.0 / 112);
+  const F step = range > size ? range : size;
+  F s;
+  if constexpr (WIDE) {
+    s = step < 0x1p-14 ? __builtin_ceil(step * 0x1p17) * 0x1p-17
+                       : __longlong_as_double((__double_as_longlong(step) + ((1LL << 49) - 1)) & ~((1LL << 49) - 1));
+  } else {
+    const float wide = step * 0x1p17f, off = error * 0x1p15f + wide * 0x1p-21f;  // (of step: a seventh of twice the error)
+    if (step < 0x1p-14f) {
+      s = __builtin_ceilf(wide) * 0x1p-17f;
+      *unsure = step > 0.0f && fabsf(wide - __builtin_rintf(wide)) <= off;
+    } else {
+      s = __int_as_float((__float_as_int(step) + 0xfffff) & ~0xfffff);
+      const float below = __int_as_float(__float_as_int(step) & ~0xfffff);  // the nearest such numbers on either side
+      *unsure = (step - below) * 0x1p17f <= off || (s - step) * 0x1p17f <= off;
+    }
+  }
+  const F over = s > 0 ? s : (F)1, r = (F)1 / over;
+  const F z = -__builtin_rint(kv4_quotient(lo, over, r));
+  const F doubt = (F)0.5 - error * r * (F)1.0625 - (error > 0 ? most * r * (F)0x1p-21 : (F)0);
   uint32_t word = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    double n = __builtin_rint(kv4_quotient(v[e], over, r)) + z;
+    const F t = kv4_quotient(v[e], over, r), whole = WIDE ? __builtin_rint(t) : __builtin_rintf(t);
+    if (!WIDE && error > 0) *unsure |= fabsf(t - whole) >= doubt;
+    F n = whole + z;
     n = n < 0 ? 0 : (n > 15 ? 15 : n);
     word |= (uint32_t)(int)n << (4 * e);
   }

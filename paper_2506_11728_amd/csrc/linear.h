@@ -65,8 +65,13 @@ struct LinearColumns {
 };
 __device__ __forceinline__ LinearColumns linear_columns(const LinearArgs &L, int64_t col, int64_t count) {
   LinearColumns c{{1.0f, 1.0f, 1.0f, 1.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+  if (count >= 4) {
+    if (L.col_scale) c.scale = load_real4(L.col_scale, col, REAL_F32);
+    if (L.bias) c.bias = load_real4(L.bias, col, REAL_F32);
+    return c;
+  }
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
+  for (int e = 0; e < 3; ++e) {
     if (e < count && L.col_scale) c.scale[e] = L.col_scale[col + e];
     if (e < count && L.bias) c.bias[e] = L.bias[col + e];
   }
@@ -82,14 +87,16 @@ __device__ __forceinline__ v4f linear_residual(const LinearArgs &L, int64_t row,
   return r;
 }
 
-template <int KIND>
+// STREAM: whole cache lines of a large C, which would push the operands of other workgroups out of L2 (as in the
+// other write-backs).
+template <int KIND, bool STREAM = false>
 __device__ __forceinline__ void linear_quad(const LinearArgs &L, const Activate<KIND> act, const LinearColumns &c,
                                             int64_t row, int64_t col, int64_t count, v4i sum, float row_scale, v4f residual) {
   v4f y;
 #pragma unroll
   for (int e = 0; e < 4; ++e) y[e] = act(linear_value(sum[e], row_scale, c.scale[e], c.bias[e])) + residual[e];
   if (count >= 4) {
-    store_real4(L.C, row * L.ldc + col, L.type, y);
+    store_real4<STREAM>(L.C, row * L.ldc + col, L.type, y);
   } else {
 #pragma unroll
     for (int e = 0; e < 3; ++e)
@@ -110,27 +117,37 @@ __device__ __forceinline__ void linear_one(const LinearArgs &L, int64_t row, int
   store_real(L.C, row * L.ldc + col, L.type, y);
 }
 
-// The sums of PASSES row pieces of four columns, in LDS at patch + (t * ROWS + r0) * PITCH + c0,
-// written to rows row + t * ROWS.  The residuals and the row scales are on their way before the
-// first of them is used.
-template <int KIND, int PASSES, int ROWS, int PITCH, bool FULL>
-__device__ __forceinline__ void linear_pieces(const LinearArgs &L, const Activate<KIND> act, const LinearColumns &columns,
-                                              int64_t row, int64_t rows, int64_t col, int64_t count, const int32_t *patch) {
+// What the write-back of PASSES row pieces of four columns, ROWS rows apart, needs from memory: loaded one strip of rows
+// ahead, so that its latency hides behind the strip before.
+template <int PASSES>
+struct LinearStrip {
   v4f residual[PASSES];
   float row_scale[PASSES];
-  v4i sum[PASSES];
+};
+template <int PASSES, int ROWS, bool FULL>
+__device__ __forceinline__ LinearStrip<PASSES> linear_strip(const LinearArgs &L, int64_t row, int64_t rows, int64_t col, int64_t count) {
+  LinearStrip<PASSES> s;
 #pragma unroll
   for (int t = 0; t < PASSES; ++t) {
     const bool here = (FULL || t * ROWS < rows) && count > 0;
-    residual[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    if (here && L.R) residual[t] = linear_residual(L, row + t * ROWS, col, count);
-    row_scale[t] = here && L.row_scale ? L.row_scale[row + t * ROWS] : 1.0f;
-    sum[t] = *reinterpret_cast<const v4i *>(patch + t * ROWS * PITCH);
+    s.residual[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    if (here && L.R) s.residual[t] = linear_residual(L, row + t * ROWS, col, count);
+    s.row_scale[t] = here && L.row_scale ? L.row_scale[row + t * ROWS] : 1.0f;
   }
+  return s;
+}
+// The pieces' sums are in LDS at patch + t * ROWS * PITCH.
+template <int KIND, int PASSES, int ROWS, int PITCH, bool FULL, bool STREAM>
+__device__ __forceinline__ void linear_pieces(const LinearArgs &L, const Activate<KIND> act, const LinearColumns &columns,
+                                              const LinearStrip<PASSES> &s, int64_t row, int64_t rows, int64_t col,
+                                              int64_t count, const int32_t *patch) {
+  v4i sum[PASSES];
+#pragma unroll
+  for (int t = 0; t < PASSES; ++t) sum[t] = *reinterpret_cast<const v4i *>(patch + t * ROWS * PITCH);
 #pragma unroll
   for (int t = 0; t < PASSES; ++t)
     if ((FULL || t * ROWS < rows) && count > 0)
-      linear_quad<KIND>(L, act, columns, row + t * ROWS, col, count, sum[t], row_scale[t], residual[t]);
+      linear_quad<KIND, STREAM>(L, act, columns, row + t * ROWS, col, count, sum[t], s.row_scale[t], s.residual[t]);
 }
 
 // Blocks of v_mfma_i32_16x16x64_i8 (epilogue16.h), sixteen rows at a time through the wave's patch.
@@ -144,16 +161,21 @@ __device__ __forceinline__ void store_linear16_as(const v4i (&acc)[FM][FN], cons
   const int64_t count = !active ? 0 : (FULL ? 4 : cols - c0);
   const LinearColumns columns = linear_columns(L, col0 + c0, count);
   const Activate<KIND> act = Activate<KIND>::of(L.act);
+  LinearStrip<PASSES> strip[2];
+  auto fetch = [&](int i) { return linear_strip<PASSES, ROWS, FULL>(L, row0 + i * 16 + r0, rows - (i * 16 + r0), col0 + c0, count); };
+  strip[0] = fetch(0);
 #pragma unroll
   for (int i = 0; i < FM; ++i) {
     if (!FULL && i * 16 >= rows) break;  // wave-uniform
+    if (i + 1 < FM) strip[(i + 1) & 1] = fetch(i + 1);
+    __builtin_amdgcn_sched_barrier(0);  // (the loads stay up here)
 #pragma unroll
     for (int j = 0; j < FN; ++j)
       *reinterpret_cast<v4i *>(patch + (lane & 15) * PITCH + 16 * j + 4 * (lane >> 4)) = acc[i][j];
     // same wave wrote and reads: LDS operations of a wave complete in order
     if (64 % LANES_PER_ROW != 0) asm volatile("" ::: "memory");
-    linear_pieces<KIND, PASSES, ROWS, PITCH, FULL>(L, act, columns, row0 + i * 16 + r0, rows - (i * 16 + r0), col0 + c0,
-                                                   count, patch + r0 * PITCH + c0);
+    linear_pieces<KIND, PASSES, ROWS, PITCH, FULL, FULL && FN == 8>(L, act, columns, strip[i & 1], row0 + i * 16 + r0, rows - (i * 16 + r0),
+                                                   col0 + c0, count, patch + r0 * PITCH + c0);
   }
 }
 
@@ -168,15 +190,20 @@ __device__ __forceinline__ void store_linear32_as(const v16i (&acc)[FM][FN], con
     if (!FULL && j * 32 >= cols) break;  // wave-uniform
     const int64_t count = FULL ? 4 : cols - (j * 32 + c0);
     const LinearColumns columns = linear_columns(L, col0 + j * 32 + c0, count);
+    LinearStrip<4> strip[2];
+    auto fetch = [&](int i) { return linear_strip<4, 8, FULL>(L, row0 + i * 32 + r0, rows - (i * 32 + r0), col0 + j * 32 + c0, count); };
+    strip[0] = fetch(0);
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
       if (!FULL && i * 32 >= rows) break;
+      if (i + 1 < FM) strip[(i + 1) & 1] = fetch(i + 1);
+      __builtin_amdgcn_sched_barrier(0);  // (the loads stay up here)
 #pragma unroll
       for (int q = 0; q < 4; ++q)
         *reinterpret_cast<v4i *>(patch + (lane & 31) * 36 + 8 * q + 4 * (lane >> 5)) =
             v4i{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-      linear_pieces<KIND, 4, 8, 36, FULL>(L, act, columns, row0 + i * 32 + r0, rows - (i * 32 + r0), col0 + j * 32 + c0, count,
-                                          patch + r0 * 36 + c0);
+      linear_pieces<KIND, 4, 8, 36, FULL, false>(L, act, columns, strip[i & 1], row0 + i * 32 + r0, rows - (i * 32 + r0),
+                                          col0 + j * 32 + c0, count, patch + r0 * 36 + c0);
     }
   }
 }

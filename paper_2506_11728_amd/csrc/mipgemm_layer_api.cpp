@@ -177,7 +177,13 @@ int mipgemm_attention_kv4(int64_t requests, int64_t q_heads, int64_t kv_heads, i
   P.ldq = ldq; P.ldo = ldo; P.q_rows = q_rows; P.table_stride = table_stride;
   P.pages = (int)pages; P.log_page = log2_of(page_tokens); P.kv_heads = (int)kv_heads; P.shared = (int)(q_heads / kv_heads);
   P.max_q = (int)max_q;
-  P.max_kv = pages > 0 && table_stride > 0 ? (int)max_kv : 0;  // no page can be named: no key is seen
+  if (pages == 0 || table_stride == 0) {  // no page can be named: no key is seen, and the table is not used
+    P.max_kv = 0;
+    P.block_table = q_starts;
+    P.table_stride = 1;
+  } else {
+    P.max_kv = (int)max_kv;
+  }
   P.ranges = 1; P.span = 0; P.first = 0;
   P.scale = scale;
   return static_cast<int>(mip::launch_attention(P, (int)requests, (int)head_dim, type, workspace, workspace_bytes,
