@@ -111,23 +111,32 @@ struct Kv4Reader {
 
 __device__ __forceinline__ v2h as_halves(uint32_t w) { return __builtin_bit_cast(v2h, w); }
 
+// 1024 and 64 as float16 in both halves of a word, in registers the compiler knows nothing of: as literals beside
+// their masks they would take an instruction of their own.
+struct Kv4Exponents {
+  uint32_t e1024, e64;
+  __device__ __forceinline__ Kv4Exponents() : e1024(0x64006400u), e64(0x54005400u) { asm volatile("" : "+v"(e1024), "+v"(e64)); }
+};
+
 // Steps and negated zero points of two pairs (one in either half of `pairs`).
 struct Kv4Scale {
   v2h s, z1024, z64;  // s, -(1024 + z), -(64 + z)
-  uint32_t e1024, e64;  // 1024 and 64 in both halves
+  Kv4Scale() = default;
   __device__ __forceinline__ explicit Kv4Scale(uint32_t pairs) {
-    s = as_halves((pairs & 0x00ff00ffu) << 7);
+    step(pairs);
+    zero(pairs);
+  }
+  __device__ __forceinline__ void step(uint32_t pairs) { s = as_halves((pairs & 0x00ff00ffu) << 7); }
+  __device__ __forceinline__ void zero(uint32_t pairs) {
     // z + 128 under the exponent of -1024, less the 128
     z1024 = as_halves(((pairs >> 8) & 0x00ff00ffu) ^ 0xe480e480u) + (_Float16)128.0f;
     z64 = z1024 + (_Float16)960.0f;
-    // (in registers the compiler knows nothing of: as literals, mask and exponent would take an instruction each)
-    e1024 = 0x64006400u;
-    e64 = 0x54005400u;
-    asm("" : "+v"(e1024), "+v"(e64));
   }
   // nibbles at bits 0 and 16, and at bits 4 and 20
-  __device__ __forceinline__ v2h low(uint32_t w) const { return (as_halves((w & 0x000f000fu) | e1024) + z1024) * s; }
-  __device__ __forceinline__ v2h high(uint32_t w) const { return (as_halves((w & 0x00f000f0u) | e64) + z64) * s; }
+  __device__ __forceinline__ v2h low_sum(uint32_t w, const Kv4Exponents &k) const { return as_halves((w & 0x000f000fu) | k.e1024) + z1024; }
+  __device__ __forceinline__ v2h high_sum(uint32_t w, const Kv4Exponents &k) const { return as_halves((w & 0x00f000f0u) | k.e64) + z64; }
+  __device__ __forceinline__ v2h low(uint32_t w, const Kv4Exponents &k) const { return low_sum(w, k) * s; }
+  __device__ __forceinline__ v2h high(uint32_t w, const Kv4Exponents &k) const { return high_sum(w, k) * s; }
 };
 
 __device__ __forceinline__ v8h join(v2h a, v2h b, v2h c, v2h d) {
@@ -135,9 +144,9 @@ __device__ __forceinline__ v8h join(v2h a, v2h b, v2h c, v2h d) {
 }
 
 // Operand of the scores from word w of a lane's keys: channels in the order 0 4 1 5 2 6 3 7.
-__device__ __forceinline__ v8h key_operand(uint32_t w, const Kv4Scale &g) {
+__device__ __forceinline__ v8h key_operand(uint32_t w, const Kv4Scale &g, const Kv4Exponents &k) {
   const uint32_t x = w >> 8;
-  return join(g.low(w), g.high(w), g.low(x), g.high(x));
+  return join(g.low(w, k), g.high(w, k), g.low(x, k), g.high(x, k));
 }
 
 // Operands of the output from the values of two tiles: instruction j of unit u, tokens in the order of the
@@ -152,12 +161,12 @@ struct Kv4Values {
       : g{Kv4Scale(pa[0]), Kv4Scale(pa[1]), Kv4Scale(pb[0]), Kv4Scale(pb[1])},
         selector(0x0c040c00u + (D >= 128 ? 0u : (lane & 1) * 0x00020002u)), a(a), b(b) {}
   // channels 2 k and 2 k + 1 of the lane
-  __device__ __forceinline__ void pair(int k, v8h &even, v8h &odd) const {
+  __device__ __forceinline__ void pair(int k, const Kv4Exponents &x, v8h &even, v8h &odd) const {
     const uint32_t sel = selector + k * 0x00010001u;
     const uint32_t x0 = __builtin_amdgcn_perm(a[1], a[0], sel), x1 = __builtin_amdgcn_perm(a[3], a[2], sel);
     const uint32_t x2 = __builtin_amdgcn_perm(b[1], b[0], sel), x3 = __builtin_amdgcn_perm(b[3], b[2], sel);
-    even = join(g[0].low(x0), g[1].low(x1), g[2].low(x2), g[3].low(x3));
-    odd = join(g[0].high(x0), g[1].high(x1), g[2].high(x2), g[3].high(x3));
+    even = join(g[0].low(x0, x), g[1].low(x1, x), g[2].low(x2, x), g[3].low(x3, x));
+    odd = join(g[0].high(x0, x), g[1].high(x1, x), g[2].high(x2, x), g[3].high(x3, x));
   }
 };
 
@@ -183,11 +192,11 @@ struct Pages {
   typedef const __attribute__((address_space(4))) int32_t *table_ptr;
   table_ptr table;
   const uint8_t *head;  // the head's part of page 0
-  int64_t bytes;        // from page to page
+  uint32_t bytes;       // from page to page (at most 1024 heads of 294912)
   int last, pages, log_page;
   __device__ __forceinline__ Pages(const AttentionArgs &P, int r, int of, int64_t block)
       : table((table_ptr)(uintptr_t)(P.block_table + r * P.table_stride)), head(P.cache + of * block),
-        bytes(P.kv_heads * block), last((int)P.table_stride - 1), pages(P.pages), log_page(P.log_page) {}
+        bytes((uint32_t)(P.kv_heads * block)), last((int)P.table_stride - 1), pages(P.pages), log_page(P.log_page) {}
   // What the table says of a token's page: through the scalar cache (the table is not written while a kernel reads it),
   // and asked for well ahead of the page's own loads, which would otherwise begin with a wait for it.
   __device__ __forceinline__ int of(int token) const {
@@ -199,9 +208,13 @@ struct Pages {
     return (unsigned)page < (unsigned)pages && (token >> log_page) <= last;
   }
   // the page, or one that is there to be read
-  __device__ __forceinline__ const uint8_t *part(int page, bool named) const { return head + (named ? page : 0) * bytes; }
+  __device__ __forceinline__ const uint8_t *part(int page, bool named) const { return head + (uint64_t)(uint32_t)(named ? page : 0) * bytes; }
   __device__ __forceinline__ int within(int token) const { return token & ((1 << log_page) - 1); }
 };
+
+// A range's result for a row in scratch memory: D sums, then base and sum of the softmax.
+template <int D>
+constexpr int PARTIAL = D + 4;
 
 constexpr float LOWEST = -3.402823466e38f;
 // p is 2^(score - base) in float16, base the row's maximum less HEAD when it was last set: up to 2^LIMIT before

@@ -13,10 +13,6 @@ namespace {
 
 constexpr int WAVES = 4, STEP = 32;  // keys of a wave's step: two tiles
 
-// A range's result for a row in scratch memory: D sums, then maximum and sum of the softmax.
-template <int D>
-constexpr int PARTIAL = D + 4;
-
 template <int D, int TYPE, int RT>
 __global__ __launch_bounds__(64 * WAVES, D <= 128 && RT == 1 ? 4 : 1) void attention_rows_kernel(AttentionArgs P) {
   using S = Kv4Shape<D>;
@@ -64,6 +60,7 @@ __global__ __launch_bounds__(64 * WAVES, D <= 128 && RT == 1 ? 4 : 1) void atten
 
   const _Float16 one = (_Float16)1.0f;
   const v8h ones = {one, one, one, one, one, one, one, one};
+  const Kv4Exponents exponents;
   const Kv4Reader<D> reader(P.log_page, lane);
   const int steps = end > begin ? (end - begin + STEP - 1) / STEP : 0;
   Kv4Tile<D> next[2];
@@ -95,7 +92,7 @@ __global__ __launch_bounds__(64 * WAVES, D <= 128 && RT == 1 ? 4 : 1) void atten
         const Kv4Scale g(now[u].key_pair[n] * 0x00010001u);
 #pragma unroll
         for (int w = 0; w < S::WORDS; ++w) {
-          const v8h k = key_operand(now[u].key[n][w], g);
+          const v8h k = key_operand(now[u].key[n][w], g, exponents);
 #pragma unroll
           for (int t = 0; t < RT; ++t) score[t][0][u] = multiply(k, q[t][n * S::WORDS + w], score[t][0][u]);
         }
@@ -131,7 +128,7 @@ __global__ __launch_bounds__(64 * WAVES, D <= 128 && RT == 1 ? 4 : 1) void atten
 #pragma unroll
       for (int k = 0; k < S::NIBBLES / 2; ++k) {
         v8h even, odd;
-        values.pair(k, even, odd);
+        values.pair(k, exponents, even, odd);
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
           v4f &a = out[t][n * S::NIBBLES + 2 * k], &b = out[t][n * S::NIBBLES + 2 * k + 1];
@@ -188,7 +185,7 @@ __global__ __launch_bounds__(64 * WAVES, D <= 128 && RT == 1 ? 4 : 1) void atten
   }
 }
 
-// The kernel for many rows.  A workgroup of eight waves takes 128 RT rows of one request and key head; tiles of 64 keys
+// The kernel for many rows.  A workgroup of eight waves takes 128 rows of one request and key head; tiles of 64 keys
 // are brought from codes to float16 once for all of them, each wave its share, and lie in LDS as the operands the
 // instructions take, 1 KB each, so that every read is sixteen bytes a lane in a row.
 //
@@ -196,10 +193,10 @@ __global__ __launch_bounds__(64 * WAVES, D <= 128 && RT == 1 ? 4 : 1) void atten
 // barrier after every half: while one wave keeps the matrix unit busy (output of a tile, scores of the next), the other
 // has the vector unit to itself (weights of a tile, its share of the codes to come).  Side by side they took the
 // two units in turns: 2048 queries of 32 heads over 8192 keys 335 us, NOW us apart.
-template <int D, int TYPE, int RT>
+template <int D, int TYPE>
 __global__ __launch_bounds__(512, 2) void attention_tiles_kernel(AttentionArgs P) {
   using S = Kv4Shape<D>;
-  constexpr int W = 8, TILE = 64, KEYS = 4 * S::KEY_STEPS, VALUES = 2 * S::CHANNELS;  // operands of a tile
+  constexpr int RT = 1, W = 8, TILE = 64, KEYS = 4 * S::KEY_STEPS, VALUES = 2 * S::CHANNELS;  // operands of a tile
   constexpr int KEY_PARTS = W / 4, KEY_EACH = S::KEY_STEPS / KEY_PARTS;  // a wave's share of a tile of sixteen keys
   constexpr int PAIRS = S::CHANNELS / 2, VALUE_PARTS = W / 2 < PAIRS ? W / 2 : PAIRS, VALUE_EACH = PAIRS / VALUE_PARTS;
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
@@ -248,6 +245,7 @@ __global__ __launch_bounds__(512, 2) void attention_tiles_kernel(AttentionArgs P
 
   const _Float16 one = (_Float16)1.0f;
   const v8h ones = {one, one, one, one, one, one, one, one};
+  const Kv4Exponents exponents;
   const Kv4Reader<D> reader(P.log_page, lane);
   const int tiles = end > begin ? (end - begin + TILE - 1) / TILE : 0;
   // a wave's share: keys of tile `wave % 4`, values of the tiles 2 (wave % 2) and the one after
@@ -295,7 +293,7 @@ __global__ __launch_bounds__(512, 2) void attention_tiles_kernel(AttentionArgs P
     const Kv4Scale g(key_pair * 0x00010001u);
 #pragma unroll
     for (int i = 0; i < KEY_EACH; ++i)
-      *reinterpret_cast<v8h *>(to + (key_tile * S::KEY_STEPS + key_part * KEY_EACH + i) * 1024) = key_operand(key[i], g);
+      *reinterpret_cast<v8h *>(to + (key_tile * S::KEY_STEPS + key_part * KEY_EACH + i) * 1024) = key_operand(key[i], g, exponents);
     if (key_part == 0) named[stage][key_tile] = key_named;
   };
   auto unpack_values = [&](int stage) {
@@ -310,7 +308,7 @@ __global__ __launch_bounds__(512, 2) void attention_tiles_kernel(AttentionArgs P
       const Kv4Values<D> values(second ? value[0][S::UNITS - 1] : value[0][0], second ? value[1][S::UNITS - 1] : value[1][0],
                                 second ? value_pair[0][S::UNITS - 1] : value_pair[0][0],
                                 second ? value_pair[1][S::UNITS - 1] : value_pair[1][0], lane);
-      values.pair(pair % (S::NIBBLES / 2), even, odd);
+      values.pair(pair % (S::NIBBLES / 2), exponents, even, odd);
       *reinterpret_cast<v8h *>(to + (2 * pair) * 1024) = even;
       *reinterpret_cast<v8h *>(to + (2 * pair + 1) * 1024) = odd;
     }
@@ -396,11 +394,9 @@ __global__ __launch_bounds__(512, 2) void attention_tiles_kernel(AttentionArgs P
         else multiply_tiles(std::false_type{}, std::true_type{}, 0, 0);
       }
       half_done();
-      ask(tile + ahead + 3, tile + ahead + 2);
-      if (sees_any) {
-        mask_scores(tile);
-        weights(score, scale, top, far, out, h, p);
-      }
+      if (sees_any) mask_scores(tile);
+      ask(tile + ahead + 3, tile + ahead + 2);  // (behind the scores' one read of LDS, whose wait would include it)
+      if (sees_any) weights(score, scale, top, far, out, h, p);
       unpack_values((tile + ahead) & 1);
       unpack_keys((tile + ahead + 1) & 1);
       fetch_values(tile + ahead + 1);
@@ -527,15 +523,11 @@ Cut cut_call(int64_t requests, int64_t kv_heads, int64_t shared, int head_dim, i
 template <int D, int TYPE>
 hipError_t launch_for(const AttentionArgs &P, const Cut &cut, int requests, hipStream_t s) {
   const int64_t rows = (int64_t)P.max_q * P.shared, groups = (rows + cut.rows - 1) / cut.rows * P.kv_heads;
-  constexpr int RT = D == 256 ? 1 : 2;  // (sixteen rows of 256 channels are as many registers as 32 of 128)
-  void (*kernel)(AttentionArgs);
+  AttentionKernel kernel;
   unsigned threads = 256;
   size_t lds = (size_t)WAVES * 16 * (D + 4) * 4;
   if (cut.tiles) {
-    kernel = attention_tiles_kernel<D, TYPE, 1>;
-    if constexpr (RT == 2) {
-      if (cut.rows == 256) kernel = attention_tiles_kernel<D, TYPE, RT>;
-    }
+    kernel = cut.rows == 256 ? attention_wide(D, TYPE, P.log_page) : attention_tiles_kernel<D, TYPE>;
     threads = 512;
     lds = (size_t)(D / 4) * 2048;
   } else {

@@ -14,16 +14,43 @@ namespace mip {
 
 namespace {
 
-// 1 / sqrt(x): the instruction and one step of Newton's iteration in float32.
-template <typename F>
-__device__ __forceinline__ F inverse_root(F x) {
-  if constexpr (sizeof(F) == 8) {
-    return 1.0 / __builtin_sqrt(x);
-  } else {
-    const float r = __builtin_amdgcn_rsqf(x), better = r * __builtin_fmaf(-0.5f * x * r, r, 1.5f);
-    return r > 0.0f && r < __builtin_inff() ? better : r;
-  }
+// 1 / sqrt(x): the instruction and one step of Newton's iteration.
+__device__ __forceinline__ float inverse_root(float x) {
+  const float r = __builtin_amdgcn_rsqf(x), better = r * __builtin_fmaf(-0.5f * x * r, r, 1.5f);
+  return r > 0.0f && r < __builtin_inff() ? better : r;
 }
+
+// Eight numbers as they lie in memory.
+template <int TYPE>
+struct Raw {
+  static constexpr int WORDS = TYPE == REAL_F32 ? 8 : 4;
+  uint32_t w[WORDS];
+  __device__ __forceinline__ void load(const void *from, int64_t at) {
+    const v4w *p = reinterpret_cast<const v4w *>(static_cast<const uint8_t *>(from) + at * (WORDS / 2));
+#pragma unroll
+    for (int g = 0; g < WORDS / 4; ++g) {
+      const v4w v = p[g];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[4 * g + e] = v[e];
+    }
+  }
+  __device__ __forceinline__ void load_one(const void *from, int64_t at, int e) {
+    if constexpr (TYPE == REAL_F32) w[e] = static_cast<const uint32_t *>(from)[at];
+    else w[e / 2] = (e % 2 ? w[e / 2] & 0xffff : 0) | (uint32_t)static_cast<const uint16_t *>(from)[at] << (e % 2 * 16);
+  }
+  __device__ __forceinline__ float operator[](int e) const {
+    if constexpr (TYPE == REAL_F32) return __int_as_float((int)w[e]);
+    if constexpr (TYPE == REAL_BF16) return __int_as_float((int)(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16));
+    return (float)__builtin_bit_cast(v2h, w[e / 2])[e % 2];
+  }
+  // either of two neighbours in the other's place
+  __device__ __forceinline__ Raw swapped() const {
+    Raw r;
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) r.w[i] = TYPE == REAL_F32 ? w[i ^ 1] : w[i] >> 16 | w[i] << 16;
+    return r;
+  }
+};
 
 // Where a slot's token lies: the head's part of its page, and the token's place in it.
 struct Place {
@@ -50,187 +77,193 @@ __device__ __forceinline__ void put_in_cache(const RopeArgs &P, int64_t slot, in
                                   2 * (((lane >> 2) << P.log_page) + at.token)) = (uint16_t)pair;
 }
 
-// What a lane's eight channels are turned by: y(c) cosine + y(partner) sine, the sine negative for a pair's first.
+// What becomes of a lane's eight channels but for the root: y(c) = x(c) weight cosine + x(partner) its weight sine, the sine
+// negative for a pair's first.
 struct Turn {
-  float cosine[8], sine[8];
-  int partner;  // HALVES, rot_dim a multiple of 16: the first of the channels that the lane's meet
+  float cosine[8], sine[8], own[8], other[8];
 };
-template <int D>
-__device__ __forceinline__ Turn turn_of(const RopeArgs &P, int64_t token, int c0) {
+template <bool EIGHTS>
+__device__ __forceinline__ Turn turn_of(const RopeArgs &P, int64_t token, int c0, const float *weight) {
   Turn t;
-  t.partner = 0;
+  // (worked out anew for each kind of head: its addresses, kept over the loop over heads, would take its registers)
+  asm volatile("" : "+v"(c0));
+  const int half = P.rot / 2;
+  const bool pairs = P.style == ROTATE_STYLE_PAIRS;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    t.cosine[e] = 1.0f;
+    t.cosine[e] = t.own[e] = t.other[e] = 1.0f;
     t.sine[e] = 0.0f;
   }
-  if (P.rot == 0) return t;
+  auto load8 = [](const float *from, int at, float (&to)[8]) { load_real8<REAL_F32>(from, at, to); };
+  if (weight) load8(weight, c0, t.own);
+  if (c0 >= P.rot) return t;
   const int64_t position = P.positions[token];
   const bool known = position >= 0 && position < P.table_rows;
-  const int half = P.rot / 2;
   const float *cosine = P.cosine + (known ? position : 0) * half, *sine = P.sine + (known ? position : 0) * half;
-  if (c0 < P.rot) {
-    if (P.style == ROTATE_STYLE_HALVES && half % 8 == 0) {
-      const int j = c0 < half ? c0 : c0 - half;
-      t.partner = c0 < half ? c0 + half : j;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const v4f c = load_real4(cosine, j + 4 * h, REAL_F32), s = load_real4(sine, j + 4 * h, REAL_F32);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          t.cosine[4 * h + e] = c[e];
-          t.sine[4 * h + e] = c0 < half ? -s[e] : s[e];
-        }
-      }
-    } else if (P.style == ROTATE_STYLE_PAIRS && c0 + 8 <= P.rot) {
-      const v4f c = load_real4(cosine, c0 / 2, REAL_F32), s = load_real4(sine, c0 / 2, REAL_F32);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        t.cosine[e] = c[e / 2];
-        t.sine[e] = e % 2 ? s[e / 2] : -s[e / 2];
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int c = c0 + e;
-        if (c >= P.rot) continue;
-        const bool first = P.style == ROTATE_STYLE_PAIRS ? e % 2 == 0 : c < half;
-        const int j = P.style == ROTATE_STYLE_PAIRS ? c / 2 : (first ? c : c - half);
-        t.cosine[e] = cosine[j];
-        t.sine[e] = first ? -sine[j] : sine[j];
-      }
-    }
-  }
+  auto partner = [&](int c) { return pairs ? c ^ 1 : (c < half ? c + half : c - half); };
   if (!known) {  // a position outside the table: nothing to turn by
 #pragma unroll
-    for (int e = 0; e < 8; ++e) t.cosine[e] = __builtin_nanf("");
+    for (int e = 0; e < 8; ++e)
+      if (EIGHTS || c0 + e < P.rot) t.cosine[e] = __builtin_nanf("");
+  } else if constexpr (!EIGHTS) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int c = c0 + e;
+      if (c >= P.rot) continue;
+      const bool first = pairs ? e % 2 == 0 : c < half;
+      const int j = pairs ? c / 2 : (first ? c : c - half);
+      t.cosine[e] = cosine[j];
+      t.sine[e] = first ? -sine[j] : sine[j];
+      if (weight) t.other[e] = weight[partner(c)];
+    }
+  } else if (pairs) {
+    const v4f c = load_real4(cosine, c0 / 2, REAL_F32), s = load_real4(sine, c0 / 2, REAL_F32);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      t.cosine[e] = c[e / 2];
+      t.sine[e] = e % 2 ? s[e / 2] : -s[e / 2];
+      t.other[e] = t.own[e ^ 1];
+    }
+  } else {
+    const bool first = c0 < half;
+    const int j = first ? c0 : c0 - half;
+    load8(cosine, j, t.cosine);
+    load8(sine, j, t.sine);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t.sine[e] = first ? -t.sine[e] : t.sine[e];
+    if (weight) load8(weight, partner(c0), t.other);
   }
   return t;
 }
 
-// Norm and rotation of the head whose channels 8 * lane .. + 7 are x; `row`: D numbers of LDS of its own.  Returns, for
-// float32, a bound on what its roundings can have moved a channel by: those of the sum of squares (a chain of 8 + log2
-// LANES additions), the root, two products and the rotation are below 16 of 2^-24 of the head's largest.
-template <int D, typename F>
-__device__ __forceinline__ F norm_and_rotate(const RopeArgs &P, const float *weight, const float (&gain)[8], const Turn &turn,
-                                                int lane, F (&x)[8], F *row) {
-  constexpr int LANES = D / 8;
-  const int c0 = 8 * lane;
-  if (weight) {
-    F sum = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum += x[e] * x[e];
-#pragma unroll
-    for (int d = 1; d < LANES; d *= 2) sum += __shfl_xor(sum, d);
-    const F root = inverse_root(sum * (F)(1.0 / D) + (F)P.eps);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = x[e] * root * (F)gain[e];
-  }
-  F largest = 0;
-  if constexpr (sizeof(F) == 4) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) largest = fmaxf(largest, fabsf(x[e]));
-#pragma unroll
-    for (int d = 1; d < LANES; d *= 2) largest = fmaxf(largest, __shfl_xor(largest, d));
-    largest *= 0x1p-20f;
-  }
-  if (P.rot == 0) return largest;
-  F other[8];
-  if (P.style == ROTATE_STYLE_PAIRS) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) other[e] = x[e ^ 1];
-  } else {
-    typedef F v4 __attribute__((ext_vector_type(4)));
-#pragma unroll
-    for (int g = 0; g < 2; ++g)
-      *reinterpret_cast<v4 *>(row + c0 + 4 * g) = v4{x[4 * g], x[4 * g + 1], x[4 * g + 2], x[4 * g + 3]};
-    // same wave wrote and reads: LDS operations of a wave complete in order
-    __builtin_amdgcn_wave_barrier();
-    asm volatile("" ::: "memory");
-    if (P.rot % 16 == 0) {  // (then the channels that a lane's meet are eight in a row)
-#pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        const v4 y = *reinterpret_cast<const v4 *>(row + turn.partner + 4 * g);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) other[4 * g + e] = y[e];
-      }
-    } else {
-      const int half = P.rot / 2;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int c = c0 + e;
-        other[e] = c < P.rot ? row[c < half ? c + half : c - half] : (F)0;
-      }
-    }
-    __builtin_amdgcn_wave_barrier();
-    asm volatile("" ::: "memory");
-  }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const F y = x[e] * (F)turn.cosine[e] + other[e] * (F)turn.sine[e];
-    if (c0 + e < P.rot) x[e] = y;
-  }
-  return largest;
+// The same for all lanes of a head.
+template <int LANES>
+__device__ __forceinline__ float sum_of_head(float x) {
+  x += of_lane<LANE_XOR_1>(x);
+  x += of_lane<LANE_XOR_2>(x);
+  x += of_lane<LANE_MIRROR_8>(x);
+  if (LANES > 8) x += of_lane<LANE_MIRROR_16>(x);
+  if (LANES > 16) x += __shfl_xor(x, 16);
+  return x;
 }
 
-template <int D, int TYPE>
+template <int D, int TYPE, bool EIGHTS>
 __global__ __launch_bounds__(256, 4) void rope_kernel(RopeArgs P) {
   constexpr int LANES = D / 8, HEADS = 256 / LANES;  // of a workgroup at a time
-  __shared__ __attribute__((aligned(16))) double rows[HEADS][D];
   const int lane = threadIdx.x % LANES, mine = threadIdx.x / LANES, c0 = 8 * lane;
   const int64_t token = P.token0 + blockIdx.x / P.blocks;
   const int heads = P.q_heads + (P.cache ? 2 : (P.Ko ? 1 : 0)) * P.kv_heads, step = HEADS * P.blocks;
   const int first = (int)(blockIdx.x % P.blocks) * HEADS + mine;
-  // a head's numbers are on their way while the one before is worked on
-  auto fetch = [&](int head, float (&x)[8]) {
-    const int k = head - P.q_heads, v = k - P.kv_heads;
+  const int half = P.rot / 2;
+  // A head's numbers, and those that the rotation joins to them: on their way while the head before is worked on.
+  struct Numbers { Raw<TYPE> own, other; } now = {}, next = {};
+  auto fetch = [&](int head, Numbers &x) {
     if (head >= heads) return;
-    if (k < 0) load_real8<TYPE>(P.Q, token * P.ldq + head * D + c0, x);
-    else if (v < 0) load_real8<TYPE>(P.K, token * P.ldk + k * D + c0, x);
-    else load_real8<TYPE>(P.V, token * P.ldv + v * D + c0, x);
+    const int k = head - P.q_heads, v = k - P.kv_heads;
+    const void *from = k < 0 ? P.Q : (v < 0 ? P.K : P.V);
+    const int64_t at = k < 0 ? token * P.ldq + head * D : (v < 0 ? token * P.ldk + k * D : token * P.ldv + v * D);
+    x.own.load(from, at + c0);
+    if (P.style == ROTATE_STYLE_PAIRS || c0 >= P.rot || v >= 0) return;
+    if (EIGHTS) {
+      x.other.load(from, at + (c0 < half ? c0 + half : c0 - half));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (c0 + e < P.rot) x.other.load_one(from, at + (c0 + e < half ? c0 + e + half : c0 + e - half), e);
+    }
   };
-  float next[8] = {}, q_gain[8], k_gain[8];
   fetch(first, next);
-  const Turn turn = turn_of<D>(P, token, c0);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    q_gain[e] = P.q_weight ? P.q_weight[c0 + e] : 1.0f;
-    k_gain[e] = P.k_weight ? P.k_weight[c0 + e] : 1.0f;
-  }
   const int64_t slot = P.cache ? P.slots[token] : -1;
-  for (int head = first; head < heads; head += step) {
-    float x[8];
+  auto join = [&](Numbers &x) {
+    if (P.style == ROTATE_STYLE_PAIRS) x.other = x.own.swapped();
+    if (P.rot == D) return;
+    constexpr int EACH = 8 / Raw<TYPE>::WORDS;  // (what is not rotated: not even an infinity times zero)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = next[e];
+    for (int i = 0; i < Raw<TYPE>::WORDS; ++i) x.other.w[i] = c0 + EACH * i < P.rot ? x.other.w[i] : 0;
+  };
+  float own_by[8], other_by[8];  // of the kind of head that was the last: weights and rotation in one
+  int kind = -1;
+  uint64_t again = 0, bit = 1;  // the turns (the 64th and all after it: one bit) that are to be done in float64
+  for (int head = first; head < heads; head += step, bit = bit >> 63 ? bit : bit << 1) {
+    now = next;
     fetch(head + step, next);
     const int k = head - P.q_heads, v = k - P.kv_heads;
-    if (k < 0) {
-      norm_and_rotate<D>(P, P.q_weight, q_gain, turn, lane, x, reinterpret_cast<float *>(rows[mine]));
-      store_real8<TYPE>(P.Qo, token * P.ldqo + head * D + c0, x);
+    const float *weight = k < 0 ? P.q_weight : P.k_weight;
+    if (v < 0 && kind != (k >= 0)) {
+      kind = k >= 0;
+      const Turn t = turn_of<EIGHTS>(P, token, c0, weight);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        own_by[e] = t.cosine[e] * t.own[e];
+        other_by[e] = t.sine[e] * t.other[e];
+      }
+    }
+    join(now);
+    if (P.Ko && k >= 0 && v < 0) {  // (keys that leave as numbers are worked out in float64)
+      again |= bit;
       continue;
     }
-    uint32_t word = 0, pair = 0;
-    bool unsure = P.Ko != nullptr;  // (keys that leave as numbers are worked out in float64)
-    if (!unsure) {
-      float y[8], error = 0.0f;
+    bool unsure;
+    float y[8], error = TYPE == REAL_F32 ? 1e-38f : 0.0f;  // (of values none, but in 32 bits the quotients' own rounding counts)
+    if (v < 0) {
+      // What float32's roundings can have moved a channel by: those of the sum of squares (a chain of 8 + log2 LANES
+      // additions, halved by the root), the root's, the weight's and three products' are below 20 of 2^-24 of the larger of
+      // its two terms.
+      float sum = 0.0f, largest = 0.0f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = x[e];
-      if (v < 0) error = norm_and_rotate<D>(P, P.k_weight, k_gain, turn, lane, y, reinterpret_cast<float *>(rows[mine]));
-      else if (TYPE == REAL_F32) error = 1e-38f;  // (none, but the quotients' own rounding counts)
-      word = kv4_encode(y, error, &pair, &unsure);
-    }
-    if (__any(unsure)) {
-      double y[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = x[e];
-      if (v < 0) norm_and_rotate<D>(P, P.k_weight, k_gain, turn, lane, y, rows[mine]);
-      if (v < 0 && P.Ko) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = (float)y[e];
-        store_real8<TYPE>(P.Ko, token * P.ldko + k * D + c0, x);
+      for (int e = 0; e < 8; ++e) {
+        const float x = now.own[e], p = x * own_by[e];
+        sum = __builtin_fmaf(x, x, sum);
+        y[e] = __builtin_fmaf(now.other[e], other_by[e], p);
+        largest = most3(largest, fabsf(p), fabsf(y[e]));
       }
-      word = kv4_encode(y, 0.0, &pair, &unsure);
+      const float root = weight ? inverse_root(sum_of_head<LANES>(sum) * (float)(1.0 / D) + P.eps) : 1.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] *= root;
+      if (k < 0) {
+        store_real8<TYPE>(P.Qo, token * P.ldqo + head * D + c0, y);
+        continue;
+      }
+      largest = __builtin_fmaxf(largest, of_lane<LANE_XOR_1>(largest));
+      largest = __builtin_fmaxf(largest, of_lane<LANE_XOR_2>(largest));
+      error = largest * root * 0x1.4p-20f;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = now.own[e];
     }
+    uint32_t pair, word = kv4_encode(y, error, &pair, &unsure);
+    if (__any(unsure)) again |= bit;
+    else if (P.cache) put_in_cache<D>(P, slot, v < 0 ? k : v, lane, v >= 0, word, pair);
+  }
+  if (!again) return;
+  bit = 1;
+  for (int head = first; head < heads; head += step, bit = bit >> 63 ? bit : bit << 1) {
+    const int k = head - P.q_heads, v = k - P.kv_heads;
+    if (k < 0 || !(again & bit)) continue;
+    fetch(head, now);
+    join(now);
+    double z[8];
+    if (v < 0) {
+      double sum = 0.0, root = 1.0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += (double)now.own[e] * now.own[e];
+#pragma unroll
+      for (int d = 1; d < LANES; d *= 2) sum += __shfl_xor(sum, d);
+      if (P.k_weight) root = 1.0 / __builtin_sqrt(sum * (1.0 / D) + (double)P.eps);
+      const Turn t = turn_of<EIGHTS>(P, token, c0, P.k_weight);
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        z[e] = root * ((double)now.own[e] * t.own[e] * t.cosine[e] + (double)now.other[e] * t.other[e] * t.sine[e]);
+        y[e] = (float)z[e];
+      }
+      if (P.Ko) store_real8<TYPE>(P.Ko, token * P.ldko + k * D + c0, y);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] = now.own[e];
+    }
+    uint32_t pair;
+    const uint32_t word = kv4_encode(z, &pair);
     if (P.cache) put_in_cache<D>(P, slot, v < 0 ? k : v, lane, v >= 0, word, pair);
   }
 }
@@ -282,15 +315,22 @@ hipError_t launch_tokens(void (*const (&kernels)[3][3])(ARGS), ARGS P, int64_t t
   return hipSuccess;
 }
 
+template <int D, int TYPE>
+constexpr auto rope_ones = rope_kernel<D, TYPE, false>;
+template <int D, int TYPE>
+constexpr auto rope_eights = rope_kernel<D, TYPE, true>;
+
 #define MIP_BY_TYPE(K, D) {K<D, REAL_F32>, K<D, REAL_BF16>, K<D, REAL_F16>}
 
 }  // namespace
 
 hipError_t launch_rope(const RopeArgs &P, int64_t tokens, int head_dim, int type, hipStream_t s) {
-  static void (*const kernels[3][3])(RopeArgs) = {MIP_BY_TYPE(rope_kernel, 64), MIP_BY_TYPE(rope_kernel, 128),
-                                                  MIP_BY_TYPE(rope_kernel, 256)};
+  static void (*const kernels[2][3][3])(RopeArgs) = {
+      {MIP_BY_TYPE(rope_ones, 64), MIP_BY_TYPE(rope_ones, 128), MIP_BY_TYPE(rope_ones, 256)},
+      {MIP_BY_TYPE(rope_eights, 64), MIP_BY_TYPE(rope_eights, 128), MIP_BY_TYPE(rope_eights, 256)}};
+  const bool eights = P.rot % (P.style == ROTATE_STYLE_PAIRS ? 8 : 16) == 0;
   const int heads = P.q_heads + (P.cache ? 2 : (P.Ko ? 1 : 0)) * P.kv_heads;
-  return heads ? launch_tokens(kernels, P, tokens, head_dim, type, heads, s) : hipSuccess;
+  return heads ? launch_tokens(kernels[eights], P, tokens, head_dim, type, heads, s) : hipSuccess;
 }
 
 hipError_t launch_kv4_read(const Kv4ReadArgs &P, int64_t tokens, int head_dim, int type, hipStream_t s) {

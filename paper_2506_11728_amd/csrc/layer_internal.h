@@ -43,6 +43,9 @@ struct AttentionArgs {
   int pages, log_page, kv_heads, shared, max_q, max_kv, ranges, span, first;
   float scale;
 };
+typedef void (*AttentionKernel)(AttentionArgs);
+// The kernel for 256 rows of 64 or 128 channels to a workgroup of 512 threads (8 KB of dynamic LDS to 16 channels).
+AttentionKernel attention_wide(int head_dim, int type, int log_page);
 // ranges, span, first and partials are the launcher's own; ws: scratch memory, or null.
 hipError_t launch_attention(AttentionArgs P, int requests, int head_dim, int type, void *ws, size_t ws_bytes, hipStream_t s);
 size_t attention_scratch(int64_t requests, int64_t kv_heads, int64_t shared, int head_dim, int64_t max_q, int64_t max_kv);
