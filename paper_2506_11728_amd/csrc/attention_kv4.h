@@ -102,10 +102,9 @@ struct Kv4Reader {
       pair[u] = *reinterpret_cast<const v2i *>(part + 2 * first + value_pair[u]);
     }
   }
-  __device__ __forceinline__ void load(const uint8_t *part, int first, Kv4Tile<D> &t) const {
+  __device__ __forceinline__ void load_keys(const uint8_t *part, int first, Kv4Tile<D> &t) const {
 #pragma unroll
     for (int u = 0; u < S::UNITS; ++u) load_keys<S::WORDS>(part, first, u * S::WORDS, t.key[u], t.key_pair[u]);
-    load_values(part, first, t.value, t.value_pair);
   }
 };
 

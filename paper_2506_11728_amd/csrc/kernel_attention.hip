@@ -14,14 +14,15 @@ namespace {
 constexpr int WAVES = 4, STEP = 32;  // keys of a wave's step: two tiles
 
 template <int D, int TYPE, int RT>
-__global__ __launch_bounds__(64 * WAVES, D <= 128 && RT == 1 ? 4 : 1) void attention_rows_kernel(AttentionArgs P) {
+__global__ __launch_bounds__(64 * WAVES, D <= 128 && RT == 1 ? 4 : (D == 256 && RT == 2 ? 1 : 2)) void attention_rows_kernel(AttentionArgs P) {
   using S = Kv4Shape<D>;
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   auto sums = reinterpret_cast<float (*)[16][D + 4]>(smem);  // a wave's: sixteen rows
   __shared__ float tops[WAVES][16], totals[WAVES][16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, h = lane >> 4;
-  const int range = blockIdx.x % P.ranges, of_all = P.first + blockIdx.x / P.ranges, r = blockIdx.z;
+  // (heads before ranges: neighbours go to different dies, and the ranges of short requests are empty from some on)
+  const int here = gridDim.x / P.ranges, range = blockIdx.x / here, of_all = P.first + blockIdx.x % here, r = blockIdx.z;
   const int head = of_all % P.kv_heads, tile = of_all / P.kv_heads;
   // (the first pages are on their way with the request's numbers)
   const int begin = range * P.span, mine = begin + wave * STEP;
@@ -63,23 +64,35 @@ __global__ __launch_bounds__(64 * WAVES, D <= 128 && RT == 1 ? 4 : 1) void atten
   const Kv4Exponents exponents;
   const Kv4Reader<D> reader(P.log_page, lane);
   const int steps = end > begin ? (end - begin + STEP - 1) / STEP : 0;
-  Kv4Tile<D> next[2];
-  bool named[2];  // the table names a page for the tile
-  auto fetch = [&](int step) {
+  // The codes of two tiles.  The keys of a wave's next step are on their way from its scores on, the values from its output
+  // on: where they are needed the registers are free, and four waves to a SIMD cover the rest.
+  Kv4Tile<D> now[2];
+  bool named[2] = {false, false}, known[2];  // the table names a page for the tile
+  const uint8_t *at[2];
+  int in[2];
+  auto fetch_keys = [&](int step) {
     const int token = begin + step * STEP;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int first = token + 16 * u;
       named[u] = pages.named(page[u], first);
-      reader.load(pages.part(page[u], named[u]), pages.within(first), next[u]);
+      at[u] = pages.part(page[u], named[u]);
+      in[u] = pages.within(first);
+      reader.load_keys(at[u], in[u], now[u]);
       page[u] = pages.of(first + WAVES * STEP);  // for the step after
     }
   };
-  if (wave < steps) fetch(wave);
+  auto fetch_values = [&] {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) reader.load_values(at[u], in[u], now[u].value, now[u].value_pair);
+  };
+  if (wave < steps) {
+    fetch_keys(wave);
+    fetch_values();
+  }
   for (int step = wave; step < steps; step += WAVES) {
-    Kv4Tile<D> now[2] = {next[0], next[1]};
-    const bool known[2] = {named[0], named[1]};
-    if (step + WAVES < steps) fetch(step + WAVES);
+    known[0] = named[0];
+    known[1] = named[1];
     const int token = begin + step * STEP;
 
     v4f score[RT][1][2];
@@ -98,6 +111,7 @@ __global__ __launch_bounds__(64 * WAVES, D <= 128 && RT == 1 ? 4 : 1) void atten
         }
       }
     }
+    if (step + WAVES < steps) fetch_keys(step + WAVES);
     if (token + STEP > fewest || !known[0] || !known[1]) {  // wave-uniform: some row does not see all of them
 #pragma unroll
       for (int u = 0; u < 2; ++u)
@@ -137,6 +151,7 @@ __global__ __launch_bounds__(64 * WAVES, D <= 128 && RT == 1 ? 4 : 1) void atten
         }
       }
     }
+    if (step + WAVES < steps) fetch_values();
   }
 
   // the waves' results meet: thread 16 row + part takes D / 16 channels in a row of one row
@@ -469,15 +484,28 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs P) {
     totals[group] = l;
   }
   __syncthreads();
-  if (group > 0) return;
+  if (threadIdx.x >= 64) return;
+  // the first wave: a lane takes four channels of some of the groups
+  constexpr int PARTS = 64 / LANES;
+  m = tops[0];
 #pragma unroll
-  for (int w = 1; w < GROUPS; ++w) {
-    const float top = fmaxf(m, tops[w]), a = __builtin_amdgcn_exp2f(m - top), b = __builtin_amdgcn_exp2f(tops[w] - top);
-    o = o * a + sums[w][at] * b;
-    l = l * a + totals[w] * b;
-    m = top;
+  for (int w = 1; w < GROUPS; ++w) m = fmaxf(m, tops[w]);
+  l = 0.0f;
+  o = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int w = 0; w < GROUPS / PARTS; ++w) {
+    const int of = w * PARTS + group;
+    const float by = __builtin_amdgcn_exp2f(tops[of] - m);
+    o += sums[of][at] * by;
+    l += totals[of] * by;
   }
-  store_real4(P.O, (req.q0 + query) * P.ldo + (int64_t)head * D + 4 * at, TYPE, o * (l != 0.0f ? 1.0f / l : 0.0f));
+#pragma unroll
+  for (int d = LANES; d < 64; d *= 2) {
+    l += __shfl_xor(l, d);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], d);
+  }
+  if (group == 0) store_real4(P.O, (req.q0 + query) * P.ldo + (int64_t)head * D + 4 * at, TYPE, o * (l != 0.0f ? 1.0f / l : 0.0f));
 }
 
 // `count` things, `each` workgroups to one, as many in a launch as a grid holds.
@@ -506,9 +534,19 @@ Cut cut_call(int64_t requests, int64_t kv_heads, int64_t shared, int head_dim, i
   cut.rows = rows <= 16 ? 16 : (rows <= 32 ? 32 : (rows <= 128 || head_dim == 256 ? 128 : 256));
   const int64_t groups = requests * kv_heads * ((rows + cut.rows - 1) / cut.rows);
   const int64_t round = cut.tiles ? 64 : WAVES * STEP;  // keys between two barriers, or of all waves' steps
-  int64_t want = ((cut.tiles ? 1 : 6) * compute_units() + groups - 1) / groups;
-  const int64_t least = cut.tiles ? 8 : 4;  // rounds to a range
-  const int64_t most = (max_kv + least * round - 1) / (least * round);
+  // Workgroups to a compute unit that are asked for.  Many rows: one, as many as fit.  Few rows of one request: as many as
+  // fit at once (131001 keys of 8 heads 36.5 us, 41.4 with six).  Of several, whose lengths may differ, six (32 requests of
+  // up to 8192 keys, half of them there: 44.8 us, 57.7 with four).
+  const int64_t fit = cut.tiles ? 1 : (head_dim <= 128 && cut.rows == 16 ? 4 : 2);
+  int64_t want = ((cut.tiles || requests == 1 ? fit : 6) * compute_units() + groups - 1) / groups;
+  // Rounds that a range has at least: what a workgroup begins and ends with takes as long as some of them.  While there is
+  // less than a workgroup to a compute unit, two (4096 keys 11.4 us, 12.0 with four; 5000 of 256 channels 13.7, 16.0).
+  auto ranges_of = [&](int64_t least) { return (max_kv + least * round - 1) / (least * round); };
+  int64_t most = ranges_of(cut.tiles ? 8 : 4);
+  if (!cut.tiles) {
+    const int64_t each = (compute_units() + groups - 1) / groups, fine = ranges_of(2) < each ? ranges_of(2) : each;
+    most = most > fine ? most : fine;
+  }
   if (want > most) want = most;
   if (want < 1) want = 1;
   int64_t each = (max_kv + want - 1) / want;
