@@ -78,23 +78,45 @@ __device__ __forceinline__ LinearColumns linear_columns(const LinearArgs &L, int
   return c;
 }
 
-__device__ __forceinline__ v4f linear_residual(const LinearArgs &L, int64_t row, int64_t col, int64_t count) {
-  if (count >= 4) return load_real4(L.R, row * L.ldr + col, L.type);
-  v4f r = {0.0f, 0.0f, 0.0f, 0.0f};
+// Four numbers of R as they lie in memory (in a 16-bit type: in the first two words), and what they are: a number that is
+// worked on is waited for, so what is fetched ahead stays as it came.
+__device__ __forceinline__ v4w linear_residual(const LinearArgs &L, int64_t row, int64_t col, int64_t count) {
+  const int64_t at = row * L.ldr + col;
+  v4w r = {0, 0, 0, 0};
+  if (L.type == REAL_F32) {
+    const uint32_t *from = static_cast<const uint32_t *>(L.R) + at;
+    if (count >= 4) return *reinterpret_cast<const v4w *>(from);
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < count) r[e] = from[e];
+    return r;
+  }
+  const uint16_t *from = static_cast<const uint16_t *>(L.R) + at;
+  if (count >= 4) {
+    const v2w w = *reinterpret_cast<const v2w *>(from);
+    return v4w{w[0], w[1], 0, 0};
+  }
 #pragma unroll
   for (int e = 0; e < 3; ++e)
-    if (e < count) r[e] = load_real(L.R, row * L.ldr + col + e, L.type);
+    if (e < count) r[e / 2] |= (uint32_t)from[e] << (e % 2 * 16);
   return r;
+}
+__device__ __forceinline__ v4f linear_numbers(v4w r, int type) {
+  if (type == REAL_F32) return __builtin_bit_cast(v4f, r);
+  const v2w w = {r[0], r[1]};
+  return type == REAL_BF16 ? __builtin_convertvector(__builtin_bit_cast(v4b, w), v4f)
+                           : __builtin_convertvector(__builtin_bit_cast(v4h, w), v4f);
 }
 
 // STREAM: whole cache lines of a large C, which would push the operands of other workgroups out of L2 (as in the
 // other write-backs).
 template <int KIND, bool STREAM = false>
 __device__ __forceinline__ void linear_quad(const LinearArgs &L, const Activate<KIND> act, const LinearColumns &c,
-                                            int64_t row, int64_t col, int64_t count, v4i sum, float row_scale, v4f residual) {
+                                            int64_t row, int64_t col, int64_t count, v4i sum, float row_scale, v4w residual) {
   v4f y;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) y[e] = act(linear_value(sum[e], row_scale, c.scale[e], c.bias[e])) + residual[e];
+  for (int e = 0; e < 4; ++e) y[e] = act(linear_value(sum[e], row_scale, c.scale[e], c.bias[e]));
+  if (L.R) y += linear_numbers(residual, L.type);
   if (count >= 4) {
     store_real4<STREAM>(L.C, row * L.ldc + col, L.type, y);
   } else {
@@ -121,7 +143,7 @@ __device__ __forceinline__ void linear_one(const LinearArgs &L, int64_t row, int
 // ahead, so that its latency hides behind the strip before.
 template <int PASSES>
 struct LinearStrip {
-  v4f residual[PASSES];
+  v4w residual[PASSES];
   float row_scale[PASSES];
 };
 template <int PASSES, int ROWS, bool FULL>
@@ -130,7 +152,7 @@ __device__ __forceinline__ LinearStrip<PASSES> linear_strip(const LinearArgs &L,
 #pragma unroll
   for (int t = 0; t < PASSES; ++t) {
     const bool here = (FULL || t * ROWS < rows) && count > 0;
-    s.residual[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    s.residual[t] = v4w{0, 0, 0, 0};  // (zeros in every type)
     if (here && L.R) s.residual[t] = linear_residual(L, row + t * ROWS, col, count);
     s.row_scale[t] = here && L.row_scale ? L.row_scale[row + t * ROWS] : 1.0f;
   }

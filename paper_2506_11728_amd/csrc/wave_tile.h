@@ -317,7 +317,7 @@ __global__ __launch_bounds__(64 * W) void wave_tile_kernel(
     if constexpr (UNS == LINEAR_OUT) {
       const LinearColumns columns = linear_columns(P.linear, n0 + c, cols - c);
       const float row_scale = P.linear.row_scale ? P.linear.row_scale[m0 + r] : 1.0f;
-      v4f residual = {0.0f, 0.0f, 0.0f, 0.0f};
+      v4w residual = {0, 0, 0, 0};
       if (P.linear.R) residual = linear_residual(P.linear, m0 + r, n0 + c, cols - c);
       const auto finish = [&](auto act) { linear_quad(P.linear, act, columns, m0 + r, n0 + c, cols - c, sum[u], row_scale, residual); };
       switch (activation_kind(P.linear.act)) {  // wave-uniform
