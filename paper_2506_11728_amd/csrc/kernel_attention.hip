@@ -42,17 +42,16 @@ __global__ __launch_bounds__(64 * WAVES, D <= 128 && RT == 1 ? 4 : (D == 256 && 
   bool far = true;  // (the first base is)
   int sees[RT];  // keys that the row sees
   v4f out[RT][S::CHANNELS + 1];  // the last: sums of p
+  uint32_t lost = 0;  // four bits to a row tile and unit: rows that have seen a value that is no number
   int fewest = 0x7fffffff;
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
-    const int row = row0 + 16 * t + c;
-    const bool here = row < rows;
-    const int query = here ? row / P.shared : 0;
+    // (a row that is none sees what the last one does, so that it needs no mask, and is not written)
+    const int of_row = row0 + 16 * t + c, row = of_row < rows ? of_row : rows - 1, query = row / P.shared;
     const int64_t at = (req.q0 + query) * P.ldq + (int64_t)(head * P.shared + (row - query * P.shared)) * D;
-    scale[t] = load_queries<D, TYPE>(P, at, here, h, q[t]);
-    sees[t] = here ? req.keys - req.queries + query + 1 : 0;
-    const int first_query = (row0 + 16 * t) / P.shared;
-    const int least = row0 + 16 * t + 15 < rows ? req.keys - req.queries + first_query + 1 : 0;
+    scale[t] = load_queries<D, TYPE>(P, at, of_row < rows, h, q[t]);
+    sees[t] = req.keys - req.queries + query + 1;
+    const int least = row0 + 16 * t < rows ? req.keys - req.queries + (row0 + 16 * t) / P.shared + 1 : fewest;
     fewest = least < fewest ? least : fewest;
     top[t] = LOWEST;
 #pragma unroll
@@ -136,6 +135,24 @@ __global__ __launch_bounds__(64 * WAVES, D <= 128 && RT == 1 ? 4 : (D == 256 && 
     weights(score, scale, top, far, out, h, p);
 #pragma unroll
     for (int t = 0; t < RT; ++t) out[t][S::CHANNELS] = multiply(p[t][0], ones, out[t][S::CHANNELS]);
+    if (token + STEP > fewest) {
+      uint32_t any = 0;
+#pragma unroll
+      for (int n = 0; n < S::UNITS; ++n)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) any |= no_step(now[u].value_pair[n][0]) | no_step(now[u].value_pair[n][1]);
+      if (__any(any)) {
+#pragma unroll
+        for (int n = 0; n < S::UNITS; ++n) {
+          v2i &a = now[0].value_pair[n], &b = now[1].value_pair[n];
+          const v4u none = {no_number(a[0]), no_number(a[1]), no_number(b[0]), no_number(b[1])};
+#pragma unroll
+          for (int t = 0; t < RT; ++t) lost |= seen_of(p[t][0], __builtin_bit_cast(v8h, none)) << (4 * (t * S::UNITS + n));
+          a = v2i{(int)numbers_of(a[0]), (int)numbers_of(a[1])};
+          b = v2i{(int)numbers_of(b[0]), (int)numbers_of(b[1])};
+        }
+      }
+    }
 #pragma unroll
     for (int n = 0; n < S::UNITS; ++n) {
       const Kv4Values<D> values(now[0].value[n], now[1].value[n], now[0].value_pair[n], now[1].value_pair[n], lane);
@@ -165,7 +182,8 @@ __global__ __launch_bounds__(64 * WAVES, D <= 128 && RT == 1 ? 4 : (D == 256 && 
       if (c == 0) totals[wave][4 * h + e] = out[t][S::CHANNELS][e];
 #pragma unroll
       for (int j = 0; j < S::CHANNELS; ++j)
-        sums[wave][4 * h + e][S::value_channel(j / S::NIBBLES, j % S::NIBBLES, c)] = out[t][j][e];
+        sums[wave][4 * h + e][S::value_channel(j / S::NIBBLES, j % S::NIBBLES, c)] =
+            lost >> (4 * (t * S::UNITS + j / S::NIBBLES) + e) & 1 ? __builtin_nanf("") : out[t][j][e];
     }
     __syncthreads();
     const int row = row0 + 16 * t + row_in;
@@ -200,22 +218,26 @@ __global__ __launch_bounds__(64 * WAVES, D <= 128 && RT == 1 ? 4 : (D == 256 && 
   }
 }
 
-// The kernel for many rows.  A workgroup of eight waves takes 128 rows of one request and key head; tiles of 64 keys
-// are brought from codes to float16 once for all of them, each wave its share, and lie in LDS as the operands the
+// The kernel for many rows of 256 channels.  A workgroup of eight waves takes 128 rows of one request and key head; tiles of
+// 64 keys are brought from codes to float16 once for all of them, each wave its share, and lie in LDS as the operands the
 // instructions take, 1 KB each, so that every read is sixteen bytes a lane in a row.
 //
 // A SIMD has two waves, one of either half of the workgroup, and the halves run half a tile apart, held there by a
 // barrier after every half: while one wave keeps the matrix unit busy (output of a tile, scores of the next), the other
-// has the vector unit to itself (weights of a tile, its share of the codes to come).  Side by side they took the
-// two units in turns: 2048 queries of 32 heads over 8192 keys 335 us, NOW us apart.
-template <int D, int TYPE>
+// has the vector unit to itself (weights of a tile, its share of the codes to come).  Side by side they take the
+// two units in turns.  2048 queries of 16 heads over 4096 keys of 4: 188 us, 550 TFLOP/s.
+template <int TYPE>
 __global__ __launch_bounds__(512, 2) void attention_tiles_kernel(AttentionArgs P) {
+  constexpr int D = 256;
   using S = Kv4Shape<D>;
   constexpr int RT = 1, W = 8, TILE = 64, KEYS = 4 * S::KEY_STEPS, VALUES = 2 * S::CHANNELS;  // operands of a tile
   constexpr int KEY_PARTS = W / 4, KEY_EACH = S::KEY_STEPS / KEY_PARTS;  // a wave's share of a tile of sixteen keys
-  constexpr int PAIRS = S::CHANNELS / 2, VALUE_PARTS = W / 2 < PAIRS ? W / 2 : PAIRS, VALUE_EACH = PAIRS / VALUE_PARTS;
+  constexpr int VALUE_EACH = S::CHANNELS / 2 / (W / 2);  // and of the values of two
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   __shared__ int named[2][4];  // whether the table names a page for the tiles of sixteen of a stage
+  // values that are no numbers: patterns of tile i % 4's steps and units, and i + 1 where there is one
+  __shared__ __attribute__((aligned(16))) uint8_t none[4][2][S::UNITS][1024];
+  __shared__ int has_none[4][2][S::UNITS];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, h = lane >> 4;
   const int range = blockIdx.x % P.ranges, r = blockIdx.z;
@@ -242,31 +264,31 @@ __global__ __launch_bounds__(512, 2) void attention_tiles_kernel(AttentionArgs P
   bool far = true;  // (the first base is)
   int sees[RT];
   v4f out[RT][S::CHANNELS + 1];  // the last: sums of p
+  uint32_t lost = 0;  // four bits to a row tile and unit: rows that have seen a value that is no number
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
-    const int row = wave_row + 16 * t + c;
-    const bool here = row < rows;
-    const int query = here ? row / P.shared : 0;
+    const int of_row = wave_row + 16 * t + c, row = of_row < rows ? of_row : rows - 1, query = row / P.shared;
     const int64_t at = (req.q0 + query) * P.ldq + (int64_t)(head * P.shared + (row - query * P.shared)) * D;
-    scale[t] = load_queries<D, TYPE>(P, at, here, h, q[t]);
-    sees[t] = here ? before + query : 0;
+    scale[t] = load_queries<D, TYPE>(P, at, of_row < rows, h, q[t]);
+    sees[t] = before + query;
     top[t] = LOWEST;
 #pragma unroll
     for (int j = 0; j <= S::CHANNELS; ++j) out[t][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
   }
   // the fewest and the most keys that a row of the wave sees
   const int wave_end = wave_row + 16 * RT < rows ? wave_row + 16 * RT : rows;
-  const int fewest = wave_row + 16 * RT <= rows ? sees_of(wave_row) : 0, most = wave_row < rows ? sees_of(wave_end - 1) : 0;
+  const int fewest = wave_row < rows ? sees_of(wave_row) : 0, most = wave_row < rows ? sees_of(wave_end - 1) : 0;
 
   const _Float16 one = (_Float16)1.0f;
   const v8h ones = {one, one, one, one, one, one, one, one};
   const Kv4Exponents exponents;
   const Kv4Reader<D> reader(P.log_page, lane);
   const int tiles = end > begin ? (end - begin + TILE - 1) / TILE : 0;
-  // a wave's share: keys of tile `wave % 4`, values of the tiles 2 (wave % 2) and the one after
+  // a wave's share: keys of tile `wave % 4`, a quarter of the channels of the values of the tiles 2 (wave % 2) and the one after
+  const int unit = value_part * VALUE_EACH / (S::NIBBLES / 2);
   uint32_t key[KEY_EACH], key_pair;
-  v4u value[2][S::UNITS];
-  v2i value_pair[2][S::UNITS];
+  v4u value[2];
+  v2i value_pair[2];
   bool key_named;
   // (past the last tile, the last again: what it becomes is not used)
   auto first_of = [&](int tile) { return begin + (tile < tiles ? tile : tiles - 1) * TILE; };
@@ -293,14 +315,11 @@ __global__ __launch_bounds__(512, 2) void attention_tiles_kernel(AttentionArgs P
     for (int i = 0; i < 2; ++i) {
       const int first = first_of(tile) + 32 * step + 16 * i;
       const bool exists = pages.named(value_page[i], first);
-      reader.load_values(pages.part(value_page[i], exists), pages.within(first), value[i], value_pair[i]);
+      reader.load_values(pages.part(value_page[i], exists), pages.within(first), unit, value[i], value_pair[i]);
       // what lies behind the last key, and in pages that are none, is no number: a step of zero makes it zero
       const int exist = exists ? end - first - 4 * h : 0;
-#pragma unroll
-      for (int n = 0; n < S::UNITS; ++n) {
-        if (exist < 4) value_pair[i][n][1] &= exist < 3 ? 0 : 0x0000ffff;
-        if (exist < 2) value_pair[i][n][0] &= exist < 1 ? 0 : 0x0000ffff;
-      }
+      if (exist < 4) value_pair[i][1] &= exist < 3 ? 0 : 0x0000ffff;
+      if (exist < 2) value_pair[i][0] &= exist < 1 ? 0 : 0x0000ffff;
     }
   };
   auto unpack_keys = [&](int stage) {
@@ -311,18 +330,25 @@ __global__ __launch_bounds__(512, 2) void attention_tiles_kernel(AttentionArgs P
       *reinterpret_cast<v8h *>(to + (key_tile * S::KEY_STEPS + key_part * KEY_EACH + i) * 1024) = key_operand(key[i], g, exponents);
     if (key_part == 0) named[stage][key_tile] = key_named;
   };
-  auto unpack_values = [&](int stage) {
-    if (value_part >= VALUE_PARTS) return;
+  auto unpack_values = [&](int tile) {
+    const int stage = tile & 1;
+    if (tile < tiles && begin + tile * TILE + TILE > sees_of(row0)) {  // some row may not see all of its keys
+      v2i &a = value_pair[0], &b = value_pair[1];
+      if (__any(no_step(a[0]) | no_step(a[1]) | no_step(b[0]) | no_step(b[1]))) {  // (two waves find and write the same)
+        has_none[tile & 3][step][unit] = tile + 1;
+        int at = 16 * lane;
+        asm volatile("" : "+v"(at));  // (its addresses are not kept over the loop)
+        *reinterpret_cast<v4u *>(none[tile & 3][step][unit] + at) = v4u{no_number(a[0]), no_number(a[1]), no_number(b[0]), no_number(b[1])};
+        a = v2i{(int)numbers_of(a[0]), (int)numbers_of(a[1])};
+        b = v2i{(int)numbers_of(b[0]), (int)numbers_of(b[1])};
+      }
+    }
     uint8_t *to = smem + (2 * KEYS + stage * VALUES + step * S::CHANNELS) * 1024 + 16 * lane;
+    const Kv4Values<D> values(value[0], value[1], value_pair[0], value_pair[1], lane);
 #pragma unroll
     for (int i = 0; i < VALUE_EACH; ++i) {
-      const int pair = value_part * VALUE_EACH + i, n = VALUE_EACH * VALUE_PARTS == PAIRS && S::UNITS == 1 ? 0 : pair / (S::NIBBLES / 2);
+      const int pair = value_part * VALUE_EACH + i;
       v8h even, odd;
-      // (a unit's registers by a wave-uniform choice)
-      const bool second = S::UNITS == 2 && n == 1;
-      const Kv4Values<D> values(second ? value[0][S::UNITS - 1] : value[0][0], second ? value[1][S::UNITS - 1] : value[1][0],
-                                second ? value_pair[0][S::UNITS - 1] : value_pair[0][0],
-                                second ? value_pair[1][S::UNITS - 1] : value_pair[1][0], lane);
       values.pair(pair % (S::NIBBLES / 2), exponents, even, odd);
       *reinterpret_cast<v8h *>(to + (2 * pair) * 1024) = even;
       *reinterpret_cast<v8h *>(to + (2 * pair + 1) * 1024) = odd;
@@ -334,7 +360,7 @@ __global__ __launch_bounds__(512, 2) void attention_tiles_kernel(AttentionArgs P
   // LOOK before it is used, in this order and no other, since left to itself the compiler reads two and waits for
   // them.
   auto multiply_tiles = [&](auto values_tag, auto keys_tag, int value_stage, int key_stage) {
-    constexpr int V = decltype(values_tag)::value ? VALUES : 0, N = V + (decltype(keys_tag)::value ? KEYS : 0), LOOK = 4;
+    constexpr int V = decltype(values_tag)::value ? VALUES : 0, N = V + (decltype(keys_tag)::value ? KEYS : 0), LOOK = 3;
     const uint8_t *values = smem + (2 * KEYS + value_stage * VALUES) * 1024 + 16 * lane;
     const uint8_t *keys = smem + key_stage * (KEYS * 1024) + 16 * lane;
     auto read = [&](int i) { return *reinterpret_cast<const v8h *>(i < V ? values + i * 1024 : keys + (i - V) * 1024); };
@@ -357,6 +383,22 @@ __global__ __launch_bounds__(512, 2) void attention_tiles_kernel(AttentionArgs P
       }
       if (i + LOOK < N) ring[i % LOOK] = read(i + LOOK);
       __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // NaN in the rows that see a value of the tile that is no number
+  auto mark_none = [&](int tile) {
+    if (begin + tile * TILE + TILE <= sees_of(row0)) return;  // (the others' keys count too: what is made zero is for all)
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+      for (int n = 0; n < S::UNITS; ++n) {
+        if (__builtin_amdgcn_readfirstlane(has_none[tile & 3][half][n]) != tile + 1) continue;
+        int at = 16 * lane;
+        asm volatile("" : "+v"(at));
+        const v8h pattern = *reinterpret_cast<const v8h *>(none[tile & 3][half][n] + at);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) lost |= seen_of(p[t][half], pattern) << (4 * (t * S::UNITS + n));
+      }
     }
   };
   auto mask_scores = [&](int tile) {
@@ -383,6 +425,7 @@ __global__ __launch_bounds__(512, 2) void attention_tiles_kernel(AttentionArgs P
   // and the keys of i + 1 in half 2 i + 1, the others the same in half 2 i, ahead of it by a tile: after the last
   // reads of what they overwrite, before the first of theirs.
   const int ahead = wave >> 2;
+  if (tid < 8 * S::UNITS) has_none[tid & 3][tid >> 2 & 1][tid >> 3] = 0;
   if (tiles > 0) {
     ask(1, 1);
     fetch_keys(0);
@@ -412,14 +455,15 @@ __global__ __launch_bounds__(512, 2) void attention_tiles_kernel(AttentionArgs P
       if (sees_any) mask_scores(tile);
       ask(tile + ahead + 3, tile + ahead + 2);  // (behind the scores' one read of LDS, whose wait would include it)
       if (sees_any) weights(score, scale, top, far, out, h, p);
-      unpack_values((tile + ahead) & 1);
+      unpack_values(tile + ahead);
       unpack_keys((tile + ahead + 1) & 1);
       fetch_values(tile + ahead + 1);
       fetch_keys(tile + ahead + 2);
       told();
       half_done();
       // (the rows of a wave that see nothing of the next tile end here)
-      if (sees_any && (tile + 1 == tiles || begin + (tile + 1) * TILE >= most)) 
+      if (sees_any) mark_none(tile);
+      if (sees_any && (tile + 1 == tiles || begin + (tile + 1) * TILE >= most))
         multiply_tiles(std::true_type{}, std::false_type{}, tile & 1, 0);
     }
     if (!ahead) half_done();
@@ -443,7 +487,8 @@ __global__ __launch_bounds__(512, 2) void attention_tiles_kernel(AttentionArgs P
       }
 #pragma unroll
       for (int j = 0; j < S::CHANNELS; j += 4) {
-        const v4f o = v4f{out[t][j][e], out[t][j + 1][e], out[t][j + 2][e], out[t][j + 3][e]} * by;
+        const v4f o = v4f{out[t][j][e], out[t][j + 1][e], out[t][j + 2][e], out[t][j + 3][e]} *
+                      (lost >> (4 * (t * S::UNITS + j / S::NIBBLES) + e) & 1 ? __builtin_nanf("") : by);
         const int channel = S::value_channel(j / S::NIBBLES, j % S::NIBBLES, c);
         if (P.partials) *reinterpret_cast<v4f *>(to + channel) = o;
         else store_real4(P.O, at + channel, TYPE, o);
@@ -530,8 +575,11 @@ struct Cut {
 Cut cut_call(int64_t requests, int64_t kv_heads, int64_t shared, int head_dim, int64_t max_q, int64_t max_kv) {
   const int64_t rows = max_q * shared;
   Cut cut;
-  cut.tiles = rows > 32;
-  cut.rows = rows <= 16 ? 16 : (rows <= 32 ? 32 : (rows <= 128 || head_dim == 256 ? 128 : 256));
+  // The kernels for many rows bring a tile of keys to float16 once for all of them, but begin with barriers and little
+  // to a compute unit: 8 requests of up to 8192 keys, 96 rows of 128 channels, 49 us here and 73 there; 256 rows 97 and 88.
+  // In 256 channels, where few registers are left for a second workgroup, 36 rows 97 here and 83 there.
+  cut.tiles = rows > (head_dim == 256 ? 32 : 128);
+  cut.rows = cut.tiles ? (head_dim == 256 ? 128 : 256) : (rows <= 16 ? 16 : 32);
   const int64_t groups = requests * kv_heads * ((rows + cut.rows - 1) / cut.rows);
   const int64_t round = cut.tiles ? 64 : WAVES * STEP;  // keys between two barriers, or of all waves' steps
   // Workgroups to a compute unit that are asked for.  Many rows: one, as many as fit.  Few rows of one request: as many as
@@ -565,13 +613,15 @@ hipError_t launch_for(const AttentionArgs &P, const Cut &cut, int requests, hipS
   unsigned threads = 256;
   size_t lds = (size_t)WAVES * 16 * (D + 4) * 4;
   if (cut.tiles) {
-    kernel = cut.rows == 256 ? attention_wide(D, TYPE, P.log_page) : attention_tiles_kernel<D, TYPE>;
+    if constexpr (D == 256) kernel = attention_tiles_kernel<TYPE>;
+    else kernel = attention_wide(D, TYPE, P.log_page);
     threads = 512;
     lds = (size_t)(D / 4) * 2048;
   } else {
     kernel = cut.rows == 16 ? attention_rows_kernel<D, TYPE, 1> : attention_rows_kernel<D, TYPE, 2>;
   }
-  hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(kernel), lds + 1024);  // (and what is not dynamic)
+  // (in 256 channels what is not dynamic leaves just that much)
+  hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(kernel), lds + (D == 256 ? 0 : 18432));
   if (e == hipSuccess) e = launch_in_slabs(kernel, P, groups, P.ranges, requests, threads, lds, s);
   if (e != hipSuccess || !P.partials) return e;
   return launch_in_slabs(attention_join_kernel<D, TYPE>, P, (int64_t)P.max_q * P.kv_heads * P.shared, 1, requests, 256, 0, s);

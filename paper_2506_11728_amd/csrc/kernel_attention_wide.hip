@@ -38,6 +38,9 @@ __global__ __launch_bounds__(512, 2) void attention_wide_kernel(AttentionArgs P)
   constexpr bool FOLD = TYPE == REAL_BF16;
   constexpr float FAR = FOLD ? 32768.0f : 1048576.0f;  // past what float16 holds, or float32 with fractions
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+  // values that are no numbers: patterns of tile i % 4's sixteens, and i + 1 for a sixteen that has one
+  __shared__ __attribute__((aligned(16))) uint8_t none[4][4][1024];
+  __shared__ int has_none[4][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 31, h = lane >> 5;
   const int range = blockIdx.x % P.ranges, r = blockIdx.z;
@@ -61,12 +64,12 @@ __global__ __launch_bounds__(512, 2) void attention_wide_kernel(AttentionArgs P)
   if (range > 0 && begin >= end) return;
 
   // queries: lane's row, channels D / 2 h + 8 i + 0 4 1 5 2 6 3 7 in operand i
-  const int wave_row = row0 + 32 * wave, row = wave_row + c;
-  const bool here = row < rows;
-  const int query = here ? row / P.shared : 0;
-  const int sees = here ? before + query : 0;
+  // (a row that is none sees what the last one does, so that it needs no mask, and is not written)
+  const int wave_row = row0 + 32 * wave;
+  const bool here = wave_row + c < rows;
+  const int row = here ? wave_row + c : rows - 1, query = row / P.shared, sees = before + query;
   // the fewest and the most keys that a row of the wave sees
-  const int fewest = wave_row + 32 <= rows ? sees_of(wave_row) : 0;
+  const int fewest = wave_row < rows ? sees_of(wave_row) : 0;
   const int most = wave_row < rows ? sees_of((wave_row + 32 < rows ? wave_row + 32 : rows) - 1) : 0;
   v8h q[KEY_STEPS];
   float back;  // what a score is multiplied by to be an exponent
@@ -138,6 +141,7 @@ __global__ __launch_bounds__(512, 2) void attention_wide_kernel(AttentionArgs P)
   const int tiles = end > begin ? (end - begin + TILE - 1) / TILE : 0;
   // whether the table names all the pages that are read here (if not, every tile asks it again)
   bool whole = true;
+  if (tid < 16) has_none[tid >> 2][tid & 3] = 0;
   for (int i = (begin >> P.log_page) + tid; i < (end + (1 << P.log_page) - 1) >> P.log_page; i += 512)
     whole = whole && pages.named(pages.table[i < pages.last ? i : pages.last], i << P.log_page);
   whole = __syncthreads_and(whole);
@@ -191,13 +195,22 @@ __global__ __launch_bounds__(512, 2) void attention_wide_kernel(AttentionArgs P)
     }
   };
   // what lies behind the last key, and in pages that are none, is no number: a step of zero makes it zero
-  auto cut_values = [&] {
+  auto cut_values = [&](int tile) {
     if (value_room < 16) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int exist = value_room - 8 * i - 4 * h;
         if (exist < 4) value_pair[i][1] &= exist < 3 ? 0 : 0x0000ffff;
         if (exist < 2) value_pair[i][0] &= exist < 1 ? 0 : 0x0000ffff;
+      }
+    }
+    if (tile < tiles && begin + tile * TILE + TILE > sees_of(row0)) {  // some row may not see all of its keys
+      v2i &a = value_pair[0], &b = value_pair[1];
+      if (__any(no_step(a[0]) | no_step(a[1]) | no_step(b[0]) | no_step(b[1]))) {  // (two waves find and write the same)
+        has_none[tile & 3][unit] = tile + 1;
+        *reinterpret_cast<v4u *>(none[tile & 3][unit] + 16 * lane) = v4u{no_number(a[0]), no_number(a[1]), no_number(b[0]), no_number(b[1])};
+        a = v2i{(int)numbers_of(a[0]), (int)numbers_of(a[1])};
+        b = v2i{(int)numbers_of(b[0]), (int)numbers_of(b[1])};
       }
     }
   };
@@ -300,6 +313,19 @@ __global__ __launch_bounds__(512, 2) void attention_wide_kernel(AttentionArgs P)
       __builtin_amdgcn_sched_barrier(0);
     }
   };
+  // NaN in the rows that see a value of the tile that is no number
+  auto mark_none = [&](int tile) {
+    if (begin + tile * TILE + TILE <= sees_of(row0)) return;  // (the others' keys count too: what is made zero is for all)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (__builtin_amdgcn_readfirstlane(has_none[tile & 3][u]) != tile + 1) continue;
+      const v16f count = multiply32(not_zero(p[u]), *reinterpret_cast<const v8h *>(none[tile & 3][u] + 16 * lane), all16(0.0f));
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+#pragma unroll
+        for (int j = 0; j < COLUMNS; ++j) out[j][v] = count[v] > 0.0f ? __builtin_nanf("") : out[j][v];
+    }
+  };
   auto mask_scores = [&](int tile) {
     const int token = begin + tile * TILE;
     if (token + TILE > fewest || !whole) {
@@ -396,7 +422,7 @@ __global__ __launch_bounds__(512, 2) void attention_wide_kernel(AttentionArgs P)
     place_keys(1);
     fetch_keys();
     ask(2, 1);
-    cut_values();
+    cut_values(0);
     half_done();
     told();
     if (wave >> 2) half_done();
@@ -422,10 +448,11 @@ __global__ __launch_bounds__(512, 2) void attention_wide_kernel(AttentionArgs P)
       fetch_keys();
       ask(tile + 3, tile + 2);  // (behind the scores' one read of LDS, whose wait would include it)
       if (sees_any) weights();
-      cut_values();
+      cut_values(tile + 1);
       told();
       half_done();
       // (the rows of a wave that see nothing of the next tile end here)
+      if (sees_any) mark_none(tile);
       if (sees_any && (tile + 1 == tiles || begin + (tile + 1) * TILE >= most))
         multiply_tiles(std::true_type{}, std::false_type{}, tile & 1, 0, [](int) {});
     }

@@ -500,3 +500,68 @@ def test_attention_in_a_graph_over_growing_lengths(gpu):
             call(eager.zero_())
         side.synchronize()
         assert torch.equal(out, eager), n
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("queries", [1, 3, 9, 40, 200])
+def test_a_value_that_is_no_number_reaches_only_what_sees_it(gpu, d, queries):
+    """A group of a value that is NaN makes its 32 channels NaN where the token is seen, and changes nothing elsewhere."""
+    import torch
+    page, hkv, heads, keys = 32, 2, 8, 333
+    c = Cached([keys, 50], hkv, d, page, seed=7)
+    q = torch.randn((queries + 1, heads, d), generator=torch.Generator().manual_seed(8)).to(torch.bfloat16)
+    clean = c.run(gpu, q, [queries, 1], BF16, d ** -0.5)
+    assert torch.isfinite(clean).all()
+    block, lost = page * d // 8 * 9, torch.zeros(clean.shape, dtype=torch.bool, device="cuda")
+    for token, kv, g in ((keys - 1, 0, 0), (keys - queries // 2 - 1, 1, d // 32 - 1), (keys - queries, 1, 1), (keys - queries - 70, 0, 1)):
+        if token < 0:
+            continue
+        slot = int(c.rows[0][token])
+        c.cache.view(-1)[(slot // page * hkv + kv) * block + page * d // 16 * 17 + 2 * (g * page + slot % page)] = 0xFF
+        first = max(token - (keys - queries), 0)  # the first query that sees it
+        lost[first:queries, kv * (heads // hkv):(kv + 1) * (heads // hkv), 32 * g:32 * g + 32] = True
+    for split in (True, False):
+        got = c.run(gpu, q, [queries, 1], BF16, d ** -0.5, split=split)
+        same = clean if split else got
+        assert torch.equal(torch.isnan(got), lost), split
+        assert torch.equal(got[~lost], same[~lost])
+        want = clean[~lost]
+        assert float((got[~lost] - want).norm() / want.norm()) <= 2.0 ** -7
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("page", [16, 32, 64, 256])
+@pytest.mark.parametrize("queries", [1, 20, 150])
+def test_pages_that_are_none(gpu, d, page, queries):
+    """Keys of pages that the table does not name are not seen, whatever the number of rows."""
+    import torch
+    keys = 5 * page + 7
+    queries = min(queries, keys)
+    c = Cached([keys], 2, d, page, seed=9)
+    q = torch.randn((queries, 8, d), generator=torch.Generator().manual_seed(10)).to(torch.float16)
+    full = c.rows[0].clone()
+    c.table[0, 1], c.table[0, 4] = -1, 2 ** 30
+    got = c.run(gpu, q, [queries], F16, d ** -0.5)
+    at = torch.arange(keys)
+    there = (at // page != 1) & (at // page != 4)
+    for i in range(queries):
+        seen = there & (at <= keys - queries + i)
+        if i not in (0, 1, queries // 2, queries - 1):
+            continue
+        slots = full[seen].cuda()
+        for h in range(8):
+            want = R.attention(q[i:i + 1, h].double().cuda(), c.keys[slots, h // 4], c.values[slots, h // 4], d ** -0.5)
+            assert float((got[i, h] - want[0]).norm()) <= 2.0 ** -8 * float(c.values.abs().amax()) * d ** 0.5
+
+
+def test_a_query_that_is_no_number_among_many(gpu):
+    import torch
+    c = Cached([500], 1, 128, 64, seed=11)
+    q = torch.randn((300, 2, 128), generator=torch.Generator().manual_seed(12)).to(torch.bfloat16)
+    clean = c.run(gpu, q, [300], BF16, 0.1)
+    q[7, 1, 5], q[250, 0, 0] = float("nan"), float("inf")
+    got = c.run(gpu, q, [300], BF16, 0.1)
+    bad = torch.isnan(got).all(-1)
+    assert bad[7, 1] and bad[250, 0] and int(bad.sum()) == 2
+    # (the rows that share a wave with them take their queries unscaled: rounded otherwise, to no fewer bits)
+    assert float((got[~bad] - clean[~bad]).norm() / clean[~bad].norm()) <= 2.0 ** -7
