@@ -63,16 +63,16 @@ struct Kv4Tile {
 template <int D>
 struct Kv4Reader {
   using S = Kv4Shape<D>;
-  int key, key_pair[S::UNITS], value, value_pair[S::UNITS];  // bytes
+  uint32_t key, key_pair[S::UNITS], value, value_pair[S::UNITS];  // bytes
   __device__ __forceinline__ Kv4Reader(int log_page, int lane) {
     const int c = lane & 15, h = lane >> 4, page = 1 << log_page;
     const Kv4Layout L(page, D);
     key = c * (D / 2) + h * (4 * S::WORDS);
-    value = (int)L.values + 16 * (h * (D / 8) + (D >= 128 ? c : c >> 1));
+    value = (uint32_t)L.values + 16 * (h * (D / 8) + (D >= 128 ? c : c >> 1));
 #pragma unroll
     for (int u = 0; u < S::UNITS; ++u) {
-      key_pair[u] = (int)L.key_pairs + 2 * (((D >= 128 ? 4 * u + h : h >> 1) << log_page) + c);
-      value_pair[u] = (int)L.value_pairs + 2 * (((D >= 128 ? 4 * u + (c >> 2) : c >> 3) << log_page) + 4 * h);
+      key_pair[u] = (uint32_t)L.key_pairs + 2 * (((D >= 128 ? 4 * u + h : h >> 1) << log_page) + c);
+      value_pair[u] = (uint32_t)L.value_pairs + 2 * (((D >= 128 ? 4 * u + (c >> 2) : c >> 3) << log_page) + 4 * h);
     }
   }
   // COUNT words of a key from instruction `from` on (all of them of one unit), and its group's pair

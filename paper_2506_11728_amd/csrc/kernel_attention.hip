@@ -588,10 +588,11 @@ Cut cut_call(int64_t requests, int64_t kv_heads, int64_t shared, int head_dim, i
   const int64_t fit = cut.tiles ? 1 : (head_dim <= 128 && cut.rows == 16 ? 4 : 2);
   int64_t want = ((cut.tiles || requests == 1 ? fit : 6) * compute_units() + groups - 1) / groups;
   // Rounds that a range has at least: what a workgroup begins and ends with takes as long as some of them.  While there is
-  // less than a workgroup to a compute unit, two (4096 keys 11.4 us, 12.0 with four; 5000 of 256 channels 13.7, 16.0).
+  // less than a workgroup to a compute unit, two (4096 keys 11.4 us, 12.0 with four; 5000 of 256 channels 13.7, 16.0), but four and less stay whole
+  // (301 keys 6.4 us, 10.3 in two, of which joining them is 3).
   auto ranges_of = [&](int64_t least) { return (max_kv + least * round - 1) / (least * round); };
   int64_t most = ranges_of(cut.tiles ? 8 : 4);
-  if (!cut.tiles) {
+  if (!cut.tiles && most > 1) {
     const int64_t each = (compute_units() + groups - 1) / groups, fine = ranges_of(2) < each ? ranges_of(2) : each;
     most = most > fine ? most : fine;
   }

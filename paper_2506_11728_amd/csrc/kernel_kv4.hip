@@ -59,22 +59,27 @@ struct Place {
 };
 template <int D>
 __device__ __forceinline__ Place place_of(uint8_t *cache, int64_t slot, int log_page, int kv_heads, int head) {
-  const int64_t block = ((int64_t)D / 8 * 9) << log_page;
-  return {cache + ((slot >> log_page) * kv_heads + head) * block, (int)(slot & ((1 << log_page) - 1))};
+  const uint32_t block = (uint32_t)(D / 8 * 9) << log_page;  // (1024 heads of it stay below 2^32)
+  return {cache + (slot >> log_page) * (int64_t)(block * (uint32_t)kv_heads) + block * (uint32_t)head, (int)(slot & ((1 << log_page) - 1))};
+}
+// Bytes from there to a lane's word of codes, and to its group's pair.
+template <int D>
+__device__ __forceinline__ uint32_t word_at(int token, int lane, bool value, int log_page) {
+  const uint32_t values = (uint32_t)(D / 16 * 9) << log_page;
+  return value ? values + 16 * ((token >> 2) * (D / 8) + lane) + 4 * (token & 3) : (uint32_t)(token * (D / 2) + 4 * lane);
+}
+template <int D>
+__device__ __forceinline__ uint32_t pair_at(int token, int lane, bool value, int log_page) {
+  return ((uint32_t)(value ? D / 16 * 17 : D / 2) << log_page) + 2 * (((lane >> 2) << log_page) + token);
 }
 
 template <int D>
 __device__ __forceinline__ void put_in_cache(const RopeArgs &P, int64_t slot, int head, int lane, bool value, uint32_t word,
                                              uint32_t pair) {
   if (slot < 0 || slot >= P.pages << P.log_page) return;
-  const Kv4Layout L(1 << P.log_page, D);
   const Place at = place_of<D>(P.cache, slot, P.log_page, P.kv_heads, head);
-  uint8_t *codes = at.part + (value ? L.values + 16 * ((at.token >> 2) * (D / 8) + lane) + 4 * (at.token & 3)
-                                    : at.token * (D / 2) + 4 * lane);
-  *reinterpret_cast<uint32_t *>(codes) = word;
-  if ((lane & 3) == 0)
-    *reinterpret_cast<uint16_t *>(at.part + (value ? L.value_pairs : L.key_pairs) +
-                                  2 * (((lane >> 2) << P.log_page) + at.token)) = (uint16_t)pair;
+  *reinterpret_cast<uint32_t *>(at.part + word_at<D>(at.token, lane, value, P.log_page)) = word;
+  if ((lane & 3) == 0) *reinterpret_cast<uint16_t *>(at.part + pair_at<D>(at.token, lane, value, P.log_page)) = (uint16_t)pair;
 }
 
 // What becomes of a lane's eight channels but for the root: y(c) = x(c) weight cosine + x(partner) its weight sine, the sine
@@ -147,65 +152,82 @@ __device__ __forceinline__ float sum_of_head(float x) {
   return x;
 }
 
+// EIGHTS: a lane's eight channels meet eight in a row, or are none that are rotated (the number of rotated channels is a
+// multiple of 16, of 8 in pairs); else they are looked for one by one.
 template <int D, int TYPE, bool EIGHTS>
-__global__ __launch_bounds__(256, 4) void rope_kernel(RopeArgs P) {
-  constexpr int LANES = D / 8, HEADS = 256 / LANES;  // of a workgroup at a time
-  const int lane = threadIdx.x % LANES, mine = threadIdx.x / LANES, c0 = 8 * lane;
+__global__ __launch_bounds__(256, EIGHTS && TYPE != REAL_F32 && D < 256 ? 5 : 4) void rope_kernel(RopeArgs P) {
+  constexpr int LANES = D / 8, HEADS = 64 / LANES;  // of a wave at a time, all of one kind: queries, keys or values
+  const int lane = threadIdx.x % LANES, c0 = 8 * lane, mine = threadIdx.x % 64 / LANES;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t token = P.token0 + blockIdx.x / P.blocks;
-  const int heads = P.q_heads + (P.cache ? 2 : (P.Ko ? 1 : 0)) * P.kv_heads, step = HEADS * P.blocks;
-  const int first = (int)(blockIdx.x % P.blocks) * HEADS + mine;
+  const int step = 4 * P.blocks, first = (int)(blockIdx.x % P.blocks) * 4 + wave;
+  const int q_turns = (P.q_heads + HEADS - 1) / HEADS, kv_turns = (P.kv_heads + HEADS - 1) / HEADS;
+  const int turns = q_turns + (P.cache ? 2 : (P.Ko ? 1 : 0)) * kv_turns;
   const int half = P.rot / 2;
+  const bool pairs = P.style == ROTATE_STYLE_PAIRS;
+  // A turn's kind of heads, and the lane's of them: behind the last one the last again, which is not written.
+  struct Turned { int kind, head; bool here; };
+  auto of_turn = [&](int turn) {
+    const int kind = turn < q_turns ? 0 : (turn < q_turns + kv_turns ? 1 : 2);
+    const int count = kind ? P.kv_heads : P.q_heads, head = (turn - (kind ? q_turns : 0) - (kind == 2 ? kv_turns : 0)) * HEADS + mine;
+    return Turned{kind, head < count ? head : count - 1, head < count};
+  };
   // A head's numbers, and those that the rotation joins to them: on their way while the head before is worked on.
   struct Numbers { Raw<TYPE> own, other; } now = {}, next = {};
-  auto fetch = [&](int head, Numbers &x) {
-    if (head >= heads) return;
-    const int k = head - P.q_heads, v = k - P.kv_heads;
-    const void *from = k < 0 ? P.Q : (v < 0 ? P.K : P.V);
-    const int64_t at = k < 0 ? token * P.ldq + head * D : (v < 0 ? token * P.ldk + k * D : token * P.ldv + v * D);
-    x.own.load(from, at + c0);
-    if (P.style == ROTATE_STYLE_PAIRS || c0 >= P.rot || v >= 0) return;
+  constexpr int SIZE = TYPE == REAL_F32 ? 4 : 2;
+  auto fetch = [&](int turn, Numbers &x) {
+    if (turn >= turns) return;
+    const Turned t = of_turn(turn);
+    const void *all = t.kind == 0 ? P.Q : (t.kind == 1 ? P.K : P.V);
+    const uint8_t *row = static_cast<const uint8_t *>(all) + token * (t.kind == 0 ? P.ldq : (t.kind == 1 ? P.ldk : P.ldv)) * SIZE;
+    const uint32_t at = (uint32_t)(t.head * D + c0);
+    x.own.load(row, at);
+    if (pairs || t.kind == 2) return;
     if (EIGHTS) {
-      x.other.load(from, at + (c0 < half ? c0 + half : c0 - half));
+      if (c0 < P.rot) x.other.load(row, c0 < half ? at + half : at - half);
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (c0 + e < P.rot) x.other.load_one(from, at + (c0 + e < half ? c0 + e + half : c0 + e - half), e);
+        if (c0 + e < P.rot) x.other.load_one(row, c0 + e < half ? at + e + half : at + e - half, e);
     }
   };
-  fetch(first, next);
-  const int64_t slot = P.cache ? P.slots[token] : -1;
   auto join = [&](Numbers &x) {
-    if (P.style == ROTATE_STYLE_PAIRS) x.other = x.own.swapped();
+    if (pairs) x.other = x.own.swapped();
     if (P.rot == D) return;
     constexpr int EACH = 8 / Raw<TYPE>::WORDS;  // (what is not rotated: not even an infinity times zero)
 #pragma unroll
     for (int i = 0; i < Raw<TYPE>::WORDS; ++i) x.other.w[i] = c0 + EACH * i < P.rot ? x.other.w[i] : 0;
   };
+  fetch(first, next);
+  const int64_t slot = P.cache ? P.slots[token] : -1;
+  auto write = [&](const Turned &t, const float (&y)[8]) {
+    uint8_t *row = static_cast<uint8_t *>(t.kind ? P.Ko : P.Qo) + token * (t.kind ? P.ldko : P.ldqo) * SIZE;
+    if (t.here) store_real8<TYPE>(row, (uint32_t)(t.head * D + c0), y);
+  };
   float own_by[8], other_by[8];  // of the kind of head that was the last: weights and rotation in one
-  int kind = -1;
-  uint64_t again = 0, bit = 1;  // the turns (the 64th and all after it: one bit) that are to be done in float64
-  for (int head = first; head < heads; head += step, bit = bit >> 63 ? bit : bit << 1) {
+  int known = -1;
+  uint64_t again = 0, bit = 1;  // the turns (the wave's 64th and all after it: one bit) that are to be done in float64
+  for (int turn = first; turn < turns; turn += step, bit = bit >> 63 ? bit : bit << 1) {
     now = next;
-    fetch(head + step, next);
-    const int k = head - P.q_heads, v = k - P.kv_heads;
-    const float *weight = k < 0 ? P.q_weight : P.k_weight;
-    if (v < 0 && kind != (k >= 0)) {
-      kind = k >= 0;
-      const Turn t = turn_of<EIGHTS>(P, token, c0, weight);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        own_by[e] = t.cosine[e] * t.own[e];
-        other_by[e] = t.sine[e] * t.other[e];
-      }
-    }
-    join(now);
-    if (P.Ko && k >= 0 && v < 0) {  // (keys that leave as numbers are worked out in float64)
+    fetch(turn + step, next);
+    const Turned t = of_turn(turn);
+    if (t.kind == 1 && P.Ko) {  // (keys that leave as numbers are worked out in float64)
       again |= bit;
       continue;
     }
-    bool unsure;
     float y[8], error = TYPE == REAL_F32 ? 1e-38f : 0.0f;  // (of values none, but in 32 bits the quotients' own rounding counts)
-    if (v < 0) {
+    if (t.kind < 2) {
+      const float *weight = t.kind ? P.k_weight : P.q_weight;
+      if (known != t.kind) {
+        known = t.kind;
+        const Turn by = turn_of<EIGHTS>(P, token, c0, weight);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          own_by[e] = by.cosine[e] * by.own[e];
+          other_by[e] = by.sine[e] * by.other[e];
+        }
+      }
+      join(now);
       // What float32's roundings can have moved a channel by: those of the sum of squares (a chain of 8 + log2 LANES
       // additions, halved by the root), the root's, the weight's and three products' are below 20 of 2^-24 of the larger of
       // its two terms.
@@ -215,13 +237,13 @@ __global__ __launch_bounds__(256, 4) void rope_kernel(RopeArgs P) {
         const float x = now.own[e], p = x * own_by[e];
         sum = __builtin_fmaf(x, x, sum);
         y[e] = __builtin_fmaf(now.other[e], other_by[e], p);
-        largest = most3(largest, fabsf(p), fabsf(y[e]));
+        if (t.kind) largest = most3(largest, fabsf(p), fabsf(y[e]));
       }
       const float root = weight ? inverse_root(sum_of_head<LANES>(sum) * (float)(1.0 / D) + P.eps) : 1.0f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] *= root;
-      if (k < 0) {
-        store_real8<TYPE>(P.Qo, token * P.ldqo + head * D + c0, y);
+      if (t.kind == 0) {
+        write(t, y);
         continue;
       }
       largest = __builtin_fmaxf(largest, of_lane<LANE_XOR_1>(largest));
@@ -231,40 +253,42 @@ __global__ __launch_bounds__(256, 4) void rope_kernel(RopeArgs P) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] = now.own[e];
     }
-    uint32_t pair, word = kv4_encode(y, error, &pair, &unsure);
+    uint32_t pair;
+    bool unsure;
+    const uint32_t word = kv4_encode(y, error, &pair, &unsure);
     if (__any(unsure)) again |= bit;
-    else if (P.cache) put_in_cache<D>(P, slot, v < 0 ? k : v, lane, v >= 0, word, pair);
+    else if (t.here) put_in_cache<D>(P, slot, t.head, lane, t.kind == 2, word, pair);
   }
   if (!again) return;
   bit = 1;
-  for (int head = first; head < heads; head += step, bit = bit >> 63 ? bit : bit << 1) {
-    const int k = head - P.q_heads, v = k - P.kv_heads;
-    if (k < 0 || !(again & bit)) continue;
-    fetch(head, now);
-    join(now);
+  for (int turn = first; turn < turns; turn += step, bit = bit >> 63 ? bit : bit << 1) {
+    const Turned t = of_turn(turn);
+    if (t.kind == 0 || !(again & bit)) continue;
+    fetch(turn, now);
     double z[8];
-    if (v < 0) {
+    if (t.kind == 1) {
+      join(now);
       double sum = 0.0, root = 1.0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum += (double)now.own[e] * now.own[e];
 #pragma unroll
       for (int d = 1; d < LANES; d *= 2) sum += __shfl_xor(sum, d);
       if (P.k_weight) root = 1.0 / __builtin_sqrt(sum * (1.0 / D) + (double)P.eps);
-      const Turn t = turn_of<EIGHTS>(P, token, c0, P.k_weight);
+      const Turn by = turn_of<EIGHTS>(P, token, c0, P.k_weight);
       float y[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        z[e] = root * ((double)now.own[e] * t.own[e] * t.cosine[e] + (double)now.other[e] * t.other[e] * t.sine[e]);
+        z[e] = root * ((double)now.own[e] * by.own[e] * by.cosine[e] + (double)now.other[e] * by.other[e] * by.sine[e]);
         y[e] = (float)z[e];
       }
-      if (P.Ko) store_real8<TYPE>(P.Ko, token * P.ldko + k * D + c0, y);
+      if (P.Ko) write(t, y);
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) z[e] = now.own[e];
     }
     uint32_t pair;
     const uint32_t word = kv4_encode(z, &pair);
-    if (P.cache) put_in_cache<D>(P, slot, v < 0 ? k : v, lane, v >= 0, word, pair);
+    if (P.cache && t.here) put_in_cache<D>(P, slot, t.head, lane, t.kind == 2, word, pair);
   }
 }
 
@@ -281,13 +305,9 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4ReadArgs P) {
     if (!to) continue;
     float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     if (slot >= 0 && slot < P.pages << P.log_page) {
-      const Kv4Layout L(1 << P.log_page, D);
       const Place at = place_of<D>(const_cast<uint8_t *>(P.cache), slot, P.log_page, P.kv_heads, head);
-      const uint32_t word = *reinterpret_cast<const uint32_t *>(
-          at.part + (value ? L.values + 16 * ((at.token >> 2) * (D / 8) + lane) + 4 * (at.token & 3)
-                           : at.token * (D / 2) + 4 * lane));
-      const uint32_t pair = *reinterpret_cast<const uint16_t *>(at.part + (value ? L.value_pairs : L.key_pairs) +
-                                                                2 * (((lane >> 2) << P.log_page) + at.token));
+      const uint32_t word = *reinterpret_cast<const uint32_t *>(at.part + word_at<D>(at.token, lane, value, P.log_page));
+      const uint32_t pair = *reinterpret_cast<const uint16_t *>(at.part + pair_at<D>(at.token, lane, value, P.log_page));
       const float s = kv4_step(pair);
       const int z = kv4_zero(pair);
 #pragma unroll
@@ -297,13 +317,12 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4ReadArgs P) {
   }
 }
 
-// A launch takes as many tokens as a grid holds.
+// A launch takes as many tokens as a grid holds.  groups: workgroups that a token has work for.
 template <typename ARGS>
-hipError_t launch_tokens(void (*const (&kernels)[3][3])(ARGS), ARGS P, int64_t tokens, int head_dim, int type, int heads,
+hipError_t launch_tokens(void (*const (&kernels)[3][3])(ARGS), ARGS P, int64_t tokens, int head_dim, int type, int groups,
                          hipStream_t s) {
-  const int per = 256 / (head_dim / 8);
   // a workgroup to a token, which shares what the token is turned by, where there are enough of them
-  P.blocks = tokens >= 8 * compute_units() ? 1 : (heads + per - 1) / per;
+  P.blocks = tokens >= 8 * compute_units() ? 1 : groups;
   const int64_t most = ((int64_t)1 << 23) / P.blocks > 0 ? ((int64_t)1 << 23) / P.blocks : 1;
   void (*kernel)(ARGS) = kernels[head_dim == 64 ? 0 : (head_dim == 128 ? 1 : 2)][type];
   for (int64_t t = 0; t < tokens; t += most) {
@@ -329,14 +348,15 @@ hipError_t launch_rope(const RopeArgs &P, int64_t tokens, int head_dim, int type
       {MIP_BY_TYPE(rope_ones, 64), MIP_BY_TYPE(rope_ones, 128), MIP_BY_TYPE(rope_ones, 256)},
       {MIP_BY_TYPE(rope_eights, 64), MIP_BY_TYPE(rope_eights, 128), MIP_BY_TYPE(rope_eights, 256)}};
   const bool eights = P.rot % (P.style == ROTATE_STYLE_PAIRS ? 8 : 16) == 0;
-  const int heads = P.q_heads + (P.cache ? 2 : (P.Ko ? 1 : 0)) * P.kv_heads;
-  return heads ? launch_tokens(kernels[eights], P, tokens, head_dim, type, heads, s) : hipSuccess;
+  const int per = 512 / head_dim;  // heads that a wave takes at a time
+  const int turns = (P.q_heads + per - 1) / per + (P.cache ? 2 : (P.Ko ? 1 : 0)) * ((P.kv_heads + per - 1) / per);
+  return turns ? launch_tokens(kernels[eights], P, tokens, head_dim, type, (turns + 3) / 4, s) : hipSuccess;
 }
 
 hipError_t launch_kv4_read(const Kv4ReadArgs &P, int64_t tokens, int head_dim, int type, hipStream_t s) {
   static void (*const kernels[3][3])(Kv4ReadArgs) = {MIP_BY_TYPE(kv4_read_kernel, 64), MIP_BY_TYPE(kv4_read_kernel, 128),
                                                      MIP_BY_TYPE(kv4_read_kernel, 256)};
-  return launch_tokens(kernels, P, tokens, head_dim, type, 2 * P.kv_heads, s);
+  return launch_tokens(kernels, P, tokens, head_dim, type, (2 * P.kv_heads * head_dim + 2047) / 2048, s);
 }
 
 }  // namespace mip
