@@ -662,9 +662,10 @@ size_t mipgemm_kv4_bytes(int64_t pages, int64_t page_tokens, int64_t kv_heads, i
  * example); weights are head_dim float32.  Queries go to Qo, keys to Ko (NULL: not written),
  * both rounded once from float32 or better; Qo may be Q and Ko may be K.  With a cache, each
  * token's keys, before any rounding, and values go to slot slots(token) (int64; slots of one
- * call must differ; a slot outside the cache, -1 for example, is skipped).  Keys are worked out
- * in float64 up to their codes, which so do not depend on the order of a sum.  A position
- * outside the tables makes that token's queries and keys NaN.
+ * call must differ; a slot outside the cache, -1 for example, is skipped).  Codes are those of
+ * the exact keys (where float32 leaves one in doubt they are worked out in float64), and so do
+ * not depend on the order of a sum.  A position outside the tables makes that token's queries
+ * and keys NaN.
  * Argument numbers: tokens=1 q_heads=2 kv_heads=3 head_dim=4 type=5 Q=6 ldq=7 K=8 ldk=9 V=10
  * ldv=11 q_weight=12 k_weight=13 eps=14 (finite, not negative) cosine=15 sine=16
  * table_rows=17 rot_dim=18 style=19 positions=20 Qo=21 ldqo=22 Ko=23 ldko=24 cache=25
@@ -703,7 +704,9 @@ int mipgemm_kv4_read(int64_t tokens, int64_t kv_heads, int64_t head_dim, int typ
  * h / (q_heads / kv_heads).  type is that of Q and O: MIPGEMM_BF16 or MIPGEMM_F16; rows of Q and O hold
  * all heads, ldq and ldo elements apart, and O must not overlap Q.  scale is positive.
  * Scores, softmax and sums are float32; p is rounded to float16 for the product with
- * the values.
+ * the values, and bfloat16 queries, where a key head has more than 128 rows of them, to
+ * float16 with the scale in them.  A key, a query or a group of a value that is no number makes
+ * NaN what sees it (of a value, the 32 channels of the group) and nothing else.
  *
  * The three integer arrays are read on the device alone.  q_rows (rows of Q and O), max_q
  * and max_kv are the host's upper bounds: what the arrays say beyond them is cut to them, and

@@ -171,23 +171,25 @@ struct Kv4Values {
 
 // Values that are no numbers: a step that is an infinity or NaN.  A product with them is none either, whatever it is multiplied
 // by, also by the zero of a row that does not see them: where some row of a tile does not see all of its keys they are made
-// zeros, and what sees them (p is not zero) is made NaN afterwards, by a product of two patterns of ones and zeros.
+// zeros, and what sees them is made NaN afterwards, by a product of two patterns of ones and zeros.
 //   no_number: ones, in float16, where a half of `pairs` has such a step; numbers_of: zeros there
 __device__ __forceinline__ uint32_t no_step(uint32_t pairs) { return (((pairs & 0x00ff00ffu) + 0x00080008u) >> 8) & 0x00010001u; }
 __device__ __forceinline__ uint32_t no_number(uint32_t pairs) { return no_step(pairs) * 0x3c00u; }
 __device__ __forceinline__ uint32_t numbers_of(uint32_t pairs) { return pairs & ~(no_step(pairs) * 0xffffu); }
-__device__ __forceinline__ v8h not_zero(v8h p) {
+// what a lane's row sees of its eight tokens, two times four that are APART apart: `room` of them from the first on
+template <int APART>
+__device__ __forceinline__ v8h seen_tokens(int room) {
   v8h r;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) r[e] = p[e] != (_Float16)0.0f ? (_Float16)1.0f : (_Float16)0.0f;
+  for (int e = 0; e < 8; ++e) r[e] = APART * (e / 4) + e % 4 < room ? (_Float16)1.0f : (_Float16)0.0f;
   return r;
 }
 
 __device__ __forceinline__ v4f multiply(v8h a, v8h b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-// bit e: row 4 (l / 16) + e of p sees something of the pattern's column l % 16
-__device__ __forceinline__ uint32_t seen_of(v8h p, v8h pattern) {
-  const v4f count = multiply(not_zero(p), pattern, v4f{0.0f, 0.0f, 0.0f, 0.0f});
+// bit e: row 4 (l / 16) + e sees something of the pattern's column l % 16
+__device__ __forceinline__ uint32_t seen_of(v8h tokens, v8h pattern) {
+  const v4f count = multiply(tokens, pattern, v4f{0.0f, 0.0f, 0.0f, 0.0f});
   uint32_t bits = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e) bits |= count[e] > 0.0f ? 1u << e : 0;

@@ -1,10 +1,13 @@
 // Attention over the 4-bit cache: the kernel for few rows (single tokens and drafted ones), the one for many
 // (prompts and their chunks), and the one that joins ranges of keys.
 //
-// Few rows: bound by the cache's bytes.  A workgroup takes the rows of one request and key head (16 or 32 of them) and a
-// range of its keys; its four waves take steps of 32 keys in turn, each with a running maximum, sum and
-// output of its own, which meet in LDS at the end.  Where requests and heads are too few to occupy the device the
-// keys are cut into ranges, and a second, small kernel joins them.
+// Few rows: bound by the cache's bytes where there are enough keys (one query of 32 heads over 131001 keys of 8: 31 us, 151 MB
+// at 4.9 TB/s, which is the rate of a copy; joining its 128 ranges 4.8 more), by the vector instructions that make float16 of
+// the codes where rows have to share them unevenly (32 requests of 174 to 8192 keys 39 us, 4.0 TB/s), and by first loads and
+// last sums in short calls (301 keys 6.2 us).  A workgroup takes the rows of one request and key head (16 or 32 of them; more rows,
+// more workgroups, which find the codes in L2) and a range of its keys; its four waves take steps of 32 keys in turn, each with a
+// running maximum, sum and output of its own, which meet in LDS at the end.  Where requests and heads are too few to
+// occupy the device the keys are cut into ranges, and a second, small kernel joins them.
 #include "attention_kv4.h"
 
 namespace mip {
@@ -147,7 +150,7 @@ __global__ __launch_bounds__(64 * WAVES, D <= 128 && RT == 1 ? 4 : (D == 256 && 
           v2i &a = now[0].value_pair[n], &b = now[1].value_pair[n];
           const v4u none = {no_number(a[0]), no_number(a[1]), no_number(b[0]), no_number(b[1])};
 #pragma unroll
-          for (int t = 0; t < RT; ++t) lost |= seen_of(p[t][0], __builtin_bit_cast(v8h, none)) << (4 * (t * S::UNITS + n));
+          for (int t = 0; t < RT; ++t) lost |= seen_of(seen_tokens<16>(sees[t] - (token + 4 * h)), __builtin_bit_cast(v8h, none)) << (4 * (t * S::UNITS + n));
           a = v2i{(int)numbers_of(a[0]), (int)numbers_of(a[1])};
           b = v2i{(int)numbers_of(b[0]), (int)numbers_of(b[1])};
         }
@@ -397,7 +400,7 @@ __global__ __launch_bounds__(512, 2) void attention_tiles_kernel(AttentionArgs P
         asm volatile("" : "+v"(at));
         const v8h pattern = *reinterpret_cast<const v8h *>(none[tile & 3][half][n] + at);
 #pragma unroll
-        for (int t = 0; t < RT; ++t) lost |= seen_of(p[t][half], pattern) << (4 * (t * S::UNITS + n));
+        for (int t = 0; t < RT; ++t) lost |= seen_of(seen_tokens<16>(sees[t] - (begin + tile * TILE + 32 * half + 4 * h)), pattern) << (4 * (t * S::UNITS + n));
       }
     }
   };
@@ -497,7 +500,9 @@ __global__ __launch_bounds__(512, 2) void attention_tiles_kernel(AttentionArgs P
   }
 }
 
-// The ranges of one row and head joined: a workgroup to a row, D / 4 lanes to a range, in turn.
+// The ranges of one row and head joined: a workgroup to a row, D / 4 lanes to a range, in turn, then the first wave.  Two
+// loads deep and a launch: 3 to 5 us.  (Cut by channels as well, 32 ranges at a time, 192 ranges took 39.4 us instead of 41.1
+// with the kernel before, 3 ranges of 2048 rows 34.7 instead of 29.5.)
 template <int D, int TYPE>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs P) {
   constexpr int LANES = D / 4, GROUPS = 256 / LANES;
@@ -575,9 +580,10 @@ struct Cut {
 Cut cut_call(int64_t requests, int64_t kv_heads, int64_t shared, int head_dim, int64_t max_q, int64_t max_kv) {
   const int64_t rows = max_q * shared;
   Cut cut;
-  // The kernels for many rows bring a tile of keys to float16 once for all of them, but begin with barriers and little
-  // to a compute unit: 8 requests of up to 8192 keys, 96 rows of 128 channels, 49 us here and 73 there; 256 rows 97 and 88.
-  // In 256 channels, where few registers are left for a second workgroup, 36 rows 97 here and 83 there.
+  // The kernels for many rows bring a tile of keys to float16 once for all of them, but put one workgroup on a compute unit and
+  // hold its waves together with barriers: 8 requests of up to 8192 keys, 96 rows of 128 channels, take 73 us with them and 49
+  // with the kernel for few; 256 rows 88 and 97.  In 256 channels, where the kernel for few has registers for two workgroups
+  // at most, 36 rows 83 and 97.
   cut.tiles = rows > (head_dim == 256 ? 32 : 128);
   cut.rows = cut.tiles ? (head_dim == 256 ? 128 : 256) : (rows <= 16 ? 16 : 32);
   const int64_t groups = requests * kv_heads * ((rows + cut.rows - 1) / cut.rows);

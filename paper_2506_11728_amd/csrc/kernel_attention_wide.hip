@@ -5,12 +5,17 @@
 // v_mfma_f32_32x32x16_f16, 1 KB each, so that every read is sixteen bytes a lane in a row.
 //
 // A SIMD has two waves, one of either half of the workgroup, and the halves run half a tile apart, held there by a
-// barrier after every half: while one wave keeps the matrix unit busy (output of a tile, scores of the next), the
-// other has the vector unit (weights of a tile, its share of the codes to come).  What bounds it is the vector unit:
-// beside a busy matrix unit it takes an instruction every 7 clocks (8.4 beside the 16 x 16 x 32 form, 5 alone), and
-// about 170 of them stand against 36 matrix instructions of 32 clocks a wave and tile.  In bfloat16 the scale of the scores
-// is therefore multiplied into the queries (rounded to float16's eleven bits, three more than theirs), and the base of the
-// softmax is one more term of their sums: they come out as exponents.
+// barrier after every half: while one wave keeps the matrix unit busy (output of a tile, scores of the next), the other works
+// out the weights of its tile.  A wave's share of the codes to come is unpacked between the matrix instructions, two or three
+// vector instructions after each: beside the weights it made that half twice as long as this one.  The matrix half goes before
+// the other where both could issue (290 us instead of 304).
+//
+// 2048 queries of 32 heads over 8192 keys of 8, 128 channels: 255 to 290 us by the card, 830 to 940 TFLOP/s (338 with the codes
+// beside the weights, 380 with 16 x 16 x 32 instructions and 128 rows).  What bounds it is issue: a wave and tile takes 36 matrix
+// instructions of 32 clocks, some 240 vector and 140 scalar ones, so a half takes about 2000 clocks, not the 1152 of the
+// matrix unit; and the first rows' workgroups, which see a quarter fewer keys, leave their units an eighth of the time.
+// In bfloat16 the scale of the scores is multiplied into the queries (rounded to float16's eleven bits, three more than
+// theirs), and the base of the softmax is one more term of their sums: they come out as exponents.
 //
 // Layout: lane l of an operand gives row (column) l % 32 and eight k from 8 (l / 32) on; the result has column
 // l % 32 and rows 8 (v / 4) + 4 (l / 32) + v % 4 in its sixteen registers v.
@@ -319,7 +324,7 @@ __global__ __launch_bounds__(512, 2) void attention_wide_kernel(AttentionArgs P)
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       if (__builtin_amdgcn_readfirstlane(has_none[tile & 3][u]) != tile + 1) continue;
-      const v16f count = multiply32(not_zero(p[u]), *reinterpret_cast<const v8h *>(none[tile & 3][u] + 16 * lane), all16(0.0f));
+      const v16f count = multiply32(seen_tokens<8>(sees - (begin + tile * TILE + 16 * u + 4 * h)), *reinterpret_cast<const v8h *>(none[tile & 3][u] + 16 * lane), all16(0.0f));
 #pragma unroll
       for (int v = 0; v < 16; ++v)
 #pragma unroll

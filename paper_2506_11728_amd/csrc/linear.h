@@ -3,7 +3,9 @@
 // in float32, rounded once to the type of C.  Shared by the MFMA kernels, whose LINEAR forms
 // (UNS == LINEAR_OUT) differ from the others in nothing else: the sums are complete before anything
 // is converted, in integers, and what the write-back adds to a product is the traffic of R and of
-// C, which in 16 bits is half that of int32 sums.
+// C, which in 16 bits is half that of int32 sums.  4096 x 11008 x 4096 in bfloat16: 164 us, 170 with SiLU, 192 with GELU (its
+// polynomial, with the matrix unit idle), 168 with a residual (213 when what was fetched ahead was converted as it came, and
+// so waited for); int32 results 179.
 #pragma once
 #include "epilogue16.h"
 #include "mip_internal.h"
