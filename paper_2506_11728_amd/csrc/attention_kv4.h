@@ -211,6 +211,8 @@ __device__ __forceinline__ Request request_of(const AttentionArgs &P, int r) {
   keys = keys < 0 ? 0 : (keys > P.max_kv ? P.max_kv : keys);
   return {a, (int)queries, (int)keys};
 }
+// Of so many keys those that the table can name.
+__device__ __forceinline__ int named_of(const AttentionArgs &P, int keys) { return keys < P.named_kv ? keys : P.named_kv; }
 // Where a request's keys and values of one head lie.
 struct Pages {
   typedef const __attribute__((address_space(4))) int32_t *table_ptr;

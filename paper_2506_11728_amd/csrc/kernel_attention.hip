@@ -36,7 +36,7 @@ __global__ __launch_bounds__(64 * WAVES, D <= 128 && RT == 1 ? 4 : (D == 256 && 
   if (row0 >= rows) return;
   // keys that any row of the tile sees
   const int last_query = (row0 + 16 * RT < rows ? row0 + 16 * RT - 1 : rows - 1) / P.shared;
-  const int seen = req.keys - req.queries + last_query + 1;
+  const int seen = named_of(P, req.keys - req.queries + last_query + 1);
   const int end = P.partials ? (seen < begin + P.span ? seen : begin + P.span) : seen;
   if (range > 0 && begin >= end) return;
 
@@ -257,7 +257,7 @@ __global__ __launch_bounds__(512, 2) void attention_tiles_kernel(AttentionArgs P
   if (row0 >= rows) return;
   const int before = req.keys - req.queries + 1;  // keys that the first query sees
   auto sees_of = [&](int row) { return before + row / P.shared; };
-  const int seen = sees_of(row0 + 16 * RT * W < rows ? row0 + 16 * RT * W - 1 : rows - 1);
+  const int seen = named_of(P, sees_of(row0 + 16 * RT * W < rows ? row0 + 16 * RT * W - 1 : rows - 1));
   const int end = P.partials && begin + P.span < seen ? begin + P.span : seen;
   if (range > 0 && begin >= end) return;
 
@@ -513,7 +513,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs P) {
   const int head = of_all % (P.kv_heads * P.shared), query = of_all / (P.kv_heads * P.shared);
   const Request req = request_of(P, r);
   if (query >= req.queries) return;
-  const int seen = req.keys - req.queries + query + 1;
+  const int seen = named_of(P, req.keys - req.queries + query + 1);
   // (every range that the row's tile went through has written; those that hold none of the row's keys, a sum of zero)
   const int ranges = seen <= 0 ? 1 : (seen + P.span - 1) / P.span;
   const float *from = P.partials + ((req.q0 + query) * P.kv_heads * P.shared + head) * (int64_t)P.ranges * PARTIAL<D>;

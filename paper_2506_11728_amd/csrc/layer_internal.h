@@ -41,6 +41,7 @@ struct AttentionArgs {
   float *partials;  // of split keys; null: one range
   int64_t ldq, ldo, q_rows, table_stride;
   int pages, log_page, kv_heads, shared, max_q, max_kv, ranges, span, first;
+  int named_kv;  // tokens that a row of the table can name pages for: there is nothing to be seen behind them
   float scale;
 };
 typedef void (*AttentionKernel)(AttentionArgs);

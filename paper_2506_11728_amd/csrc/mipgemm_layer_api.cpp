@@ -184,6 +184,8 @@ int mipgemm_attention_kv4(int64_t requests, int64_t q_heads, int64_t kv_heads, i
   } else {
     P.max_kv = (int)max_kv;
   }
+  const int64_t named = P.table_stride << P.log_page;
+  P.named_kv = named < P.max_kv ? (int)named : P.max_kv;
   P.ranges = 1; P.span = 0; P.first = 0;
   P.scale = scale;
   return static_cast<int>(mip::launch_attention(P, (int)requests, (int)head_dim, type, workspace, workspace_bytes,

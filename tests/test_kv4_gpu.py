@@ -565,3 +565,20 @@ def test_a_query_that_is_no_number_among_many(gpu):
     assert bad[7, 1] and bad[250, 0] and int(bad.sum()) == 2
     # (the rows that share a wave with them take their queries unscaled: rounded otherwise, to no fewer bits)
     assert float((got[~bad] - clean[~bad]).norm() / clean[~bad].norm()) <= 2.0 ** -7
+
+
+@pytest.mark.parametrize("d, queries", [(64, 1), (128, 3), (128, 170), (256, 40)])
+def test_lengths_far_beyond_the_table(gpu, d, queries):
+    """What a length says beyond the pages that a row of the table can name is not gone through."""
+    import torch
+    c = Cached([300, 37], 2, d, 16, seed=13)
+    q = torch.randn((queries + 1, 8, d), generator=torch.Generator().manual_seed(14)).to(torch.bfloat16)
+    c.lengths = [2 ** 31 - 5000, 37]
+    width = c.table.shape[1] * 16
+    for split in (True, False):
+        got = c.run(gpu, q, [queries, 1], BF16, d ** -0.5, split=split, max_kv=2 ** 31 - 5000)
+        # every query of the first request sees all of its table; what lies in the last page behind the 300 is no number
+        assert torch.isnan(got[:queries]).all()
+        want = c.exact(q[queries:], [0, 1], d ** -0.5)
+        assert float((got[queries:] - want).norm() / want.norm()) <= 2.0 ** -7
+    assert width == 304
