@@ -7,8 +7,9 @@
 // Bound by memory: x is read once, a byte an element written.  A row stays in the registers of its workgroup
 // between the reduction and the rounding where it fits (16384 numbers); longer rows are read a second time,
 // through the cache.  A wave to a row up to 1024 columns, four waves up to 4096; up to 16384 sixteen waves
-// where there is a workgroup of them at a time for every row (48 rows of 11008: 4.4 us against 6.8 with four), else four.
-// 4096 rows of 4096 in bfloat16 with a norm: 16.5 us, 50 MB at 3.0 TB/s; a row of 4096: 3.0 us, of which some 2 are the launch.
+// where there is a workgroup of them at a time for every row (48 rows of 11008: 4.2 us against 6.8 with four), else four.
+// 4096 rows of 4096 in bfloat16 with a norm: 14.6 us, 50 MB at 3.4 TB/s, a dozen vector instructions to a number; a row of
+// 4096: 3.0 us, of which some 2 are the launch.
 #include "layer_internal.h"
 #include "real.h"
 
@@ -57,12 +58,16 @@ __device__ __forceinline__ void times_weight(const QuantizeParams &P, int64_t j,
   for (int e = 0; e < 8; ++e) x[e] = __fmul_rn(x[e], w[e]);
 }
 
-// The quotient num / a for |num| <= 127 a, correctly rounded: the reciprocal r of a is, and one step of
-// Newton's iteration on the quotient then is as well (Markstein's theorem), where nothing underflows.
-__device__ __forceinline__ int code_of(float z, float a, float r) {
-  const float num = __fmul_rn(z, 127.0f);
-  const float q = num * r;
-  return (int)__builtin_rintf(__builtin_fmaf(__builtin_fmaf(-q, a, num), r, q));
+// The quotient 127 z / a, correctly rounded: the reciprocal r of a is, and one step of Newton's iteration on the quotient
+// then is as well (Markstein's theorem), where nothing underflows; then the nearest whole number, ties to even, in the
+// lowest byte (1.5 2^23 leaves no bits for fractions).
+__device__ __forceinline__ uint32_t code_of(float z, float by, float a, float r) {
+  const float num = __fmul_rn(z, by), q = num * r;
+  return __float_as_uint(__fadd_rn(__builtin_fmaf(__builtin_fmaf(-q, a, num), r, q), 12582912.0f));
+}
+// the lowest bytes of four words
+__device__ __forceinline__ uint32_t four_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
 }
 
 // WAVES to a row, ROWS rows to a workgroup; HELD: eights of columns a thread keeps, 0: none.
@@ -73,7 +78,7 @@ __global__ __launch_bounds__(64 * WAVES *ROWS) void quantize_kernel(QuantizePara
   const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS;
   const bool here = row < P.rows;
   float x[HELD ? HELD : 1][8];
-  float top = 0.0f, squares = 0.0f;
+  float top = 0.0f, squares = 0.0f, none = 0.0f;  // none: NaN where something is no number
   auto take = [&](int64_t j, float (&v)[8]) {
     load_oct<T>(P, row, j, v);
     if (P.weight) {
@@ -82,10 +87,9 @@ __global__ __launch_bounds__(64 * WAVES *ROWS) void quantize_kernel(QuantizePara
       times_weight(P, j, v);
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float m = fabsf(v[e]);
-      top = m <= top || top != top ? top : m;  // (a NaN stays)
-    }
+    for (int e = 0; e < 8; ++e) none = __builtin_fmaf(v[e], 0.0f, none);
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) top = fmaxf(fmaxf(top, fabsf(v[e])), fabsf(v[e + 1]));
   };
   if (HELD) {
 #pragma unroll
@@ -96,6 +100,7 @@ __global__ __launch_bounds__(64 * WAVES *ROWS) void quantize_kernel(QuantizePara
   } else if (here) {
     for (int64_t j = 8 * at; j < P.cols; j += 8 * THREADS) take(j, x[0]);
   }
+  if (none != 0.0f) top = __builtin_nanf("");
   auto larger = [](float a, float b) { return a != a ? a : (b <= a ? a : b); };
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
@@ -126,11 +131,13 @@ __global__ __launch_bounds__(64 * WAVES *ROWS) void quantize_kernel(QuantizePara
   }
   // far from 1, a power of two keeps the reciprocal and the products in range, and changes no quotient
   const float by = top < 0x1p-60f ? 0x1p60f : (top > 0x1p60f ? 0x1p-60f : 1.0f);
-  const float a = top * by, r = finite && top > 0.0f ? __fdiv_rn(1.0f, a) : 0.0f;
+  const float a = top * by, by_127 = 127.0f * by, r = finite && top > 0.0f ? __fdiv_rn(1.0f, a) : 0.0f;
   auto put = [&](int64_t j, float (&v)[8]) {
-    uint64_t word = 0;
+    uint32_t n[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) word |= (uint64_t)(uint8_t)(r != 0.0f ? code_of(v[e] * by, a, r) : 0) << (8 * e);
+    for (int e = 0; e < 8; ++e) n[e] = code_of(v[e], by_127, a, r);
+    const uint64_t both = (uint64_t)four_bytes(n[4], n[5], n[6], n[7]) << 32 | four_bytes(n[0], n[1], n[2], n[3]);
+    const uint64_t word = r != 0.0f ? both : 0;
     int8_t *q = P.Q + row * P.ldq + j;
     if (j + 8 <= P.cols) {
       reinterpret_cast<byte_oct *>(q)->v = word;
