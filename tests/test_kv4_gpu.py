@@ -582,3 +582,33 @@ def test_lengths_far_beyond_the_table(gpu, d, queries):
         want = c.exact(q[queries:], [0, 1], d ** -0.5)
         assert float((got[queries:] - want).norm() / want.norm()) <= 2.0 ** -7
     assert width == 304
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_many_rows_in_a_graph(gpu, d):
+    import torch
+    c = Cached([420, 90], 2, d, 64, seed=15)
+    queries, rows = [200, 60], 260
+    q = torch.randn((rows, 8, d), generator=torch.Generator().manual_seed(16)).to(torch.bfloat16)
+    qd, table = q.reshape(rows, -1).cuda(), c.table.cuda()
+    starts, lengths = torch.tensor([0, 200, 260], dtype=torch.int32).cuda(), torch.tensor(c.lengths, dtype=torch.int32).cuda()
+    out = torch.zeros((rows, 8 * d), dtype=torch.bfloat16, device="cuda")
+
+    def call(to):
+        gpu.mipgemm_attention_kv4(2, 8, 2, d, BF16, qd, 8 * d, rows, starts, 200, lengths, 420, c.cache, c.cache.numel(), c.pages, 64,
+                                  table, c.table.shape[1], d ** -0.5, to, 8 * d)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        call(out)
+    for n in ((420, 90), (420, 60), (300, 80)):
+        lengths.copy_(torch.tensor(n, dtype=torch.int32))
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = torch.zeros_like(out)
+        call(eager)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager), n
+        assert torch.isfinite(out).all() and float(out[199].abs().max()) > 0
