@@ -10,8 +10,9 @@ One step takes the tokens of any mix of requests, prompts and single tokens alik
     8-bit rows through the second norm  ->  first feed-forward product, bias and GELU
     8-bit rows  ->  second feed-forward product, residual
 
-ten kernels (one more where attention joins ranges of keys) and no other traffic of activations than these.  Weights are random: the sizes are those of an encoder
-block with 1024 channels, with four key heads for its sixteen query heads.
+ten kernels (one more where attention joins ranges of keys) and no other traffic of activations than these.  Weights
+are random: the sizes are those of an encoder block with 1024 channels, with four key heads for its sixteen query
+heads.
 """
 import math
 import os

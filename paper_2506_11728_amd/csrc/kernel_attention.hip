@@ -150,7 +150,10 @@ __global__ __launch_bounds__(64 * WAVES, D <= 128 && RT == 1 ? 4 : (D == 256 && 
           v2i &a = now[0].value_pair[n], &b = now[1].value_pair[n];
           const v4u none = {no_number(a[0]), no_number(a[1]), no_number(b[0]), no_number(b[1])};
 #pragma unroll
-          for (int t = 0; t < RT; ++t) lost |= seen_of(seen_tokens<16>(sees[t] - (token + 4 * h)), __builtin_bit_cast(v8h, none)) << (4 * (t * S::UNITS + n));
+          for (int t = 0; t < RT; ++t) {
+            const v8h tokens = seen_tokens<16>(sees[t] - (token + 4 * h));
+            lost |= seen_of(tokens, __builtin_bit_cast(v8h, none)) << (4 * (t * S::UNITS + n));
+          }
           a = v2i{(int)numbers_of(a[0]), (int)numbers_of(a[1])};
           b = v2i{(int)numbers_of(b[0]), (int)numbers_of(b[1])};
         }
@@ -400,7 +403,10 @@ __global__ __launch_bounds__(512, 2) void attention_tiles_kernel(AttentionArgs P
         asm volatile("" : "+v"(at));
         const v8h pattern = *reinterpret_cast<const v8h *>(none[tile & 3][half][n] + at);
 #pragma unroll
-        for (int t = 0; t < RT; ++t) lost |= seen_of(seen_tokens<16>(sees[t] - (begin + tile * TILE + 32 * half + 4 * h)), pattern) << (4 * (t * S::UNITS + n));
+        for (int t = 0; t < RT; ++t) {
+          const v8h tokens = seen_tokens<16>(sees[t] - (begin + tile * TILE + 32 * half + 4 * h));
+          lost |= seen_of(tokens, pattern) << (4 * (t * S::UNITS + n));
+        }
       }
     }
   };
@@ -594,8 +600,8 @@ Cut cut_call(int64_t requests, int64_t kv_heads, int64_t shared, int head_dim, i
   const int64_t fit = cut.tiles ? 1 : (head_dim <= 128 && cut.rows == 16 ? 4 : 2);
   int64_t want = ((cut.tiles || requests == 1 ? fit : 6) * compute_units() + groups - 1) / groups;
   // Rounds that a range has at least: what a workgroup begins and ends with takes as long as some of them.  While there is
-  // less than a workgroup to a compute unit, two (4096 keys 11.4 us, 12.0 with four; 5000 of 256 channels 13.7, 16.0), but four and less stay whole
-  // (301 keys 6.4 us, 10.3 in two, of which joining them is 3).
+  // less than a workgroup to a compute unit, two (4096 keys 11.4 us, 12.0 with four; 5000 of 256 channels 13.7, 16.0),
+  // but four and less stay whole (301 keys 6.4 us, 10.3 in two, of which joining them is 3).
   auto ranges_of = [&](int64_t least) { return (max_kv + least * round - 1) / (least * round); };
   int64_t most = ranges_of(cut.tiles ? 8 : 4);
   if (!cut.tiles && most > 1) {

@@ -289,7 +289,9 @@ __global__ __launch_bounds__(512, 2) void attention_wide_kernel(AttentionArgs P)
     constexpr int V = decltype(values_tag)::value ? VALUES : 0, N = V + (decltype(keys_tag)::value ? KEYS : 0), LOOK = 4;
     const uint8_t *values = smem + (2 * KEYS + value_stage * VALUES) * 1024 + 16 * lane;
     const uint8_t *keys = smem + key_stage * (KEYS * 1024) + 16 * lane;
-    auto read = [&](int i) { return *reinterpret_cast<const v8h *>(i < V ? values + i * 1024 : keys + ((i - V) / 2 + ((i - V) & 1) * KEY_STEPS) * 1024); };
+    auto read = [&](int i) {
+      return *reinterpret_cast<const v8h *>(i < V ? values + i * 1024 : keys + ((i - V) / 2 + ((i - V) & 1) * KEY_STEPS) * 1024);
+    };
     v8h ring[LOOK];
     // (two at a time and the second first, so that one wait is enough for both)
     auto read_two = [&](int i) {
@@ -324,7 +326,9 @@ __global__ __launch_bounds__(512, 2) void attention_wide_kernel(AttentionArgs P)
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       if (__builtin_amdgcn_readfirstlane(has_none[tile & 3][u]) != tile + 1) continue;
-      const v16f count = multiply32(seen_tokens<8>(sees - (begin + tile * TILE + 16 * u + 4 * h)), *reinterpret_cast<const v8h *>(none[tile & 3][u] + 16 * lane), all16(0.0f));
+      const v8h tokens = seen_tokens<8>(sees - (begin + tile * TILE + 16 * u + 4 * h));
+      const v8h pattern = *reinterpret_cast<const v8h *>(none[tile & 3][u] + 16 * lane);
+      const v16f count = multiply32(tokens, pattern, all16(0.0f));
 #pragma unroll
       for (int v = 0; v < 16; ++v)
 #pragma unroll

@@ -2,14 +2,17 @@
 // head of queries and keys, their rotation by position, and keys and values written to the 4-bit cache; and
 // rows of that cache read back.
 //
-// Every number is read once and written once, in one launch, so that nothing between the projection and the cache goes to
-// memory: 8192 tokens of 32 heads of queries and 8 of keys and values, 128 channels in bfloat16, would take 34 us at the rate of
-// a copy.  They take 54 (177 MB at 3.3 TB/s), bound by vector instructions: some 260 for a wave's heads, which keep the
-// SIMDs busy three quarters of the time.  d / 8 lanes to a head, eight channels to a lane: a wave takes 8, 4 or 2 heads at a time, all
-// of one kind, so that what kind they are is decided by scalar branches.  What a rotation joins to a lane's channels is loaded a
-// second time (from the first cache) rather than passed between lanes: through LDS the kernel took 88 us.  Weights and rotation
-// become one factor for each channel and its partner, once for a token and kind; the sums of squares meet in registers.  All of it is worked out in float32; where a key's code or a group's step lies so near the middle between
-// two that float32's roundings could decide it, the wave's heads are done again in float64 (some waves in a hundred): the
+// Every number is read once and written once, in one launch, so that nothing between the projection and the cache
+// goes to memory: 8192 tokens of 32 heads of queries and 8 of keys and values, 128 channels in bfloat16, would take
+// 34 us at the rate of a copy.  They take 54 (177 MB at 3.3 TB/s), bound by vector instructions: some 260 for a
+// wave's heads, which keep the SIMDs busy three quarters of the time.  d / 8 lanes to a head, eight channels to a lane:
+// a wave takes 8, 4 or 2 heads at a time, all of one kind, so that what kind they are is decided by scalar branches.
+// What a rotation joins to a lane's channels is loaded a second time (from the first cache) rather than passed between
+// lanes: through LDS the kernel took 88 us.  Weights and rotation become one factor for each channel and one for its
+// partner, once for a token and kind; the sums of squares meet in registers.
+//
+// All of it is worked out in float32; where a key's code or a group's step lies so near the middle between two that
+// float32's roundings could decide it, the wave's turn is done again in float64 (one turn in fifty to a hundred): the
 // codes are those of the exact keys, whichever order the squares are summed in.
 #include "kv4.h"
 #include "layer_internal.h"
@@ -64,7 +67,8 @@ struct Place {
 template <int D>
 __device__ __forceinline__ Place place_of(uint8_t *cache, int64_t slot, int log_page, int kv_heads, int head) {
   const uint32_t block = (uint32_t)(D / 8 * 9) << log_page;  // (1024 heads of it stay below 2^32)
-  return {cache + (slot >> log_page) * (int64_t)(block * (uint32_t)kv_heads) + block * (uint32_t)head, (int)(slot & ((1 << log_page) - 1))};
+  return {cache + (slot >> log_page) * (int64_t)(block * (uint32_t)kv_heads) + block * (uint32_t)head,
+          (int)(slot & ((1 << log_page) - 1))};
 }
 // Bytes from there to a lane's word of codes, and to its group's pair.
 template <int D>
@@ -174,7 +178,8 @@ __global__ __launch_bounds__(256, EIGHTS && TYPE != REAL_F32 && D < 256 ? 5 : 4)
   struct Turned { int kind, head; bool here; };
   auto of_turn = [&](int turn) {
     const int kind = turn < q_turns ? 0 : (turn < q_turns + kv_turns ? 1 : 2);
-    const int count = kind ? P.kv_heads : P.q_heads, head = (turn - (kind ? q_turns : 0) - (kind == 2 ? kv_turns : 0)) * HEADS + mine;
+    const int count = kind ? P.kv_heads : P.q_heads;
+    const int head = (turn - (kind ? q_turns : 0) - (kind == 2 ? kv_turns : 0)) * HEADS + mine;
     return Turned{kind, head < count ? head : count - 1, head < count};
   };
   // A head's numbers, and those that the rotation joins to them: on their way while the head before is worked on.

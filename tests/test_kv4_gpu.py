@@ -612,3 +612,40 @@ def test_many_rows_in_a_graph(gpu, d):
         torch.cuda.synchronize()
         assert torch.equal(out, eager), n
         assert torch.isfinite(out).all() and float(out[199].abs().max()) > 0
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("scale", [1.0, 40.0])
+def test_scores_far_apart_in_many_rows(gpu, d, scale):
+    """Bases that move often, and (scale 40) past what a matrix instruction takes off the scores."""
+    import torch
+    queries = [150, 200]
+    c = Cached([900, 300], 2, d, 32, seed=17, spread=30.0)
+    q = torch.randn((350, 4, d), generator=torch.Generator().manual_seed(18)).to(torch.bfloat16)
+    whole = float(np.float32(scale) * np.float32(1.4426950408889634))
+    # (of more than 128 rows of 64 or 128 channels the queries are rounded to float16 with the scale in them)
+    taken = q.double() if d == 256 else (q.float() * whole).half().double() / whole
+    want = c.exact(taken, queries, scale)
+    # scores in float32, their size times 2^-22 at most, move p by as much where two keys compete; p itself 2^-12
+    size, top = c.values.abs().amax(), float((q.double().abs().amax() * c.keys.abs().amax() * d * scale).item())
+    bound = (2.0 ** -11 + 2.0 ** -20 * (top + 4)) * size + R.rounding(want, BF16)
+    for split in (True, False):
+        got = c.run(gpu, q, queries, BF16, scale, split=split)
+        assert torch.isfinite(got).all()
+        assert ((got - want).abs() <= bound).all(), split
+        assert float((got - want).norm() / want.norm()) <= 4 * (R.UNIT[BF16] + 2.0 ** -12)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_queries_of_extreme_size_in_many_rows(gpu, d):
+    import torch
+    c = Cached([400], 1, d, 64, seed=19)
+    q = torch.randn((300, 1, d), generator=torch.Generator().manual_seed(20))
+    q[:40] *= 1e30
+    q[40:80] *= 1e-30
+    q[80:120] = 0
+    q[120:160, :, 0] = 1e20
+    q = q.to(torch.bfloat16)
+    got, want = c.run(gpu, q, [300], BF16, 0.125), c.exact(q, [300], 0.125)
+    assert torch.isfinite(got).all()
+    assert float((got - want).abs().max()) <= 2.0 ** -6 * float(want.abs().max())
