@@ -331,7 +331,8 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4ReadArgs P) {
 template <typename ARGS>
 hipError_t launch_tokens(void (*const (&kernels)[3][3])(ARGS), ARGS P, int64_t tokens, int head_dim, int type, int groups,
                          hipStream_t s) {
-  // a workgroup to a token, which shares what the token is turned by, where there are enough of them
+  // a workgroup to a token, which shares what the token is turned by, where there are enough of them (8192 tokens and
+  // their reading back 67 us, 85 with a workgroup to every four turns)
   P.blocks = tokens >= 8 * compute_units() ? 1 : groups;
   const int64_t most = ((int64_t)1 << 23) / P.blocks > 0 ? ((int64_t)1 << 23) / P.blocks : 1;
   void (*kernel)(ARGS) = kernels[head_dim == 64 ? 0 : (head_dim == 128 ? 1 : 2)][type];
