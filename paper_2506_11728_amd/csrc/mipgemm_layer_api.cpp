@@ -103,7 +103,7 @@ int mipgemm_qk_norm_rope(int64_t tokens, int64_t q_heads, int64_t kv_heads, int6
   P.q_weight = q_weight; P.k_weight = k_weight; P.cosine = cosine; P.sine = sine;
   P.positions = positions;
   P.slots = slots;
-  P.cache = static_cast<uint8_t *>(cache);
+  P.cache = kv_heads > 0 ? static_cast<uint8_t *>(cache) : nullptr;  // (without heads nothing goes there, and slots may be null)
   P.pages = pages; P.table_rows = cosine && rot_dim > 0 ? table_rows : 0; P.token0 = 0;
   P.log_page = cache ? log2_of(page_tokens) : 4;
   P.q_heads = (int)q_heads; P.kv_heads = (int)kv_heads; P.rot = (int)rot_dim; P.style = style; P.blocks = 0;

@@ -213,6 +213,21 @@ def test_queries_in_place_and_without_keys(gpu):
     assert (t.cache == 0xA5).all()
 
 
+@pytest.mark.parametrize("d", [64, 256])
+def test_queries_alone_beside_a_cache(gpu, d):
+    """Without key heads nothing goes into a cache that is given, and no slots are asked for."""
+    import torch
+    t = Heads(gpu, 70, 6, 2, d, BF16, 16, d)
+    want, _ = t.run(gpu, 0, cache=False)
+    x, qw, cos, sin, at = t.x.cuda(), t.qw.cuda(), t.cos.cuda(), t.sin.cuda(), t.positions.cuda()
+    cache = torch.full((256,), 0xA5, dtype=torch.uint8, device="cuda")
+    out = torch.full((70, 6 * d), 9.0, dtype=torch.bfloat16, device="cuda")
+    gpu.mipgemm_qk_norm_rope(70, 6, 0, d, BF16, x, t.ld, None, 1, None, 1, qw, None, 1e-5, cos, sin, 500, d, 0, at, out, 6 * d,
+                             None, 1, cache, 256, t.pages, 16, None)
+    torch.cuda.synchronize()
+    assert torch.equal(out.cpu().reshape(-1, 6, d), want) and (cache == 0xA5).all()
+
+
 # ---- attention ----
 
 class Cached:
