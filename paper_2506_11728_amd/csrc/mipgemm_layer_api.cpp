@@ -155,7 +155,7 @@ int mipgemm_attention_kv4(int64_t requests, int64_t q_heads, int64_t kv_heads, i
   if (ldq < q_heads * head_dim || ldq > MIPGEMM_MAX_DIM) return -7;
   if (q_rows < 0 || q_rows > MIPGEMM_MAX_DIM) return -8;
   if (!q_starts && any) return -9;
-  if (max_q < 0 || max_q * q_heads > MIPGEMM_MAX_DIM - 4096) return -10;
+  if (max_q < 0 || max_q > (MIPGEMM_MAX_DIM - 4096) / q_heads) return -10;  // (a product could wrap)
   if (!kv_lengths && any) return -11;
   if (max_kv < 0 || max_kv > MIPGEMM_MAX_DIM - 4096) return -12;
   if ((!cache && any && pages > 0) || reinterpret_cast<uintptr_t>(cache) % 16) return -13;

@@ -98,6 +98,16 @@ def test_refusals(M, native, monkeypatch):
         assert refused.value.code == -number
 
 
+@pytest.mark.parametrize("q_heads", [1, 2, 64, 1000, 1024])
+def test_bounds_whose_products_wrap(M, q_heads):
+    """A bound on the queries of a request that passes 64 bits, or comes back into range, times the heads is refused."""
+    more = dict(q_heads=q_heads, kv_heads=q_heads, ldq=64 * q_heads, ldo=64 * q_heads, cache_bytes=2 ** 40)
+    most = 2 ** 63 - 1
+    for max_q in (most, 2 ** 62, 2 ** 55, 2 ** 54, 2 ** 53, min(2 ** 64 // q_heads + 1, most), 2 ** 31, (2 ** 31 - 4097) // q_heads + 1):
+        assert M.mipgemm_attention_kv4(**{**ATTENTION, **more, "max_q": max_q}, stream=0, check=False) == -10, max_q
+        assert M.mipgemm_attention_kv4_workspace_size(2, q_heads, q_heads, 64, min(max_q + 4096, most), 64) == 0
+
+
 def test_empty_calls_enqueue_nothing(M):
     for name, change in [
             ("mipgemm_quantize_rows", dict(rows=0, X=None, Q=None, scales=None)),
