@@ -706,7 +706,8 @@ int mipgemm_kv4_read(int64_t tokens, int64_t kv_heads, int64_t head_dim, int typ
  * Scores, softmax and sums are float32; p is rounded to float16 for the product with
  * the values, and bfloat16 queries, where a key head has more than 128 rows of them, to
  * float16 with the scale in them.  A key, a query or a group of a value that is no number makes
- * NaN what sees it (of a value, the 32 channels of the group) and nothing else.
+ * NaN what sees it (of a value, the 32 channels of the group) and nothing else; so do scores all of which
+ * float32 cannot hold.
  *
  * The three integer arrays are read on the device alone.  q_rows (rows of Q and O), max_q
  * and max_kv are the host's upper bounds: what the arrays say beyond them is cut to them, and

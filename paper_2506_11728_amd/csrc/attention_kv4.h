@@ -236,7 +236,23 @@ struct Pages {
   // the page, or one that is there to be read
   __device__ __forceinline__ const uint8_t *part(int page, bool named) const { return head + (uint64_t)(uint32_t)(named ? page : 0) * bytes; }
   __device__ __forceinline__ int within(int token) const { return token & ((1 << log_page) - 1); }
+  // whether a row sees a key among so many tokens, none of them past the table: one whose page it names
+  __device__ __forceinline__ bool any_named(int tokens) const {
+    for (int t = 0; t < tokens; t += 1 << log_page)
+      if ((unsigned)table[t >> log_page] < (unsigned)pages) return true;
+    return false;
+  }
 };
+
+// What a row's output is multiplied by, of the sum of its p and the tokens up to its own.  The sum is zero where the row sees no
+// key, whose output is zeros, and where every score is minus infinity, which is also what masks one: those of an infinite query against
+// keys of the other sign, or past float32.  That is no number, and here, once a row, is where the two are told apart.
+__device__ __forceinline__ float of_no_sum(const AttentionArgs &P, const Pages &pages, int tokens) {
+  return pages.any_named(named_of(P, tokens)) ? __builtin_nanf("") : 0.0f;
+}
+__device__ __forceinline__ float inverse_sum(const AttentionArgs &P, const Pages &pages, float sum, int tokens) {
+  return sum != 0.0f ? 1.0f / sum : of_no_sum(P, pages, tokens);
+}
 
 // A range's result for a row in scratch memory: D sums, then base and sum of the softmax.
 template <int D>

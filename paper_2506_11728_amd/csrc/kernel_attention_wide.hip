@@ -468,10 +468,15 @@ __global__ __launch_bounds__(512, 2) void attention_wide_kernel(AttentionArgs P)
     if (!(wave >> 2)) half_done();
   }
 
+  float nothing = 0.0f;  // of a row without a sum (lane: row l % 32)
+  bool no_sum = false;
+#pragma unroll
+  for (int v = 0; v < 16; ++v) no_sum = no_sum || out[COLUMNS][v] == 0.0f;
+  if (!P.partials && __any(no_sum)) nothing = of_no_sum(P, pages, sees);
 #pragma unroll
   for (int v = 0; v < 16; ++v) {
     const int row_in = 8 * (v / 4) + 4 * h + v % 4, at_row = wave_row + row_in;
-    const float l = out[COLUMNS][v], m = __shfl(base, row_in);
+    const float l = out[COLUMNS][v], m = __shfl(base, row_in), none_of = __shfl(nothing, row_in);
     if (at_row >= rows) continue;
     const int of = at_row / P.shared, within = at_row - of * P.shared;
     float o[COLUMNS];
@@ -484,7 +489,7 @@ __global__ __launch_bounds__(512, 2) void attention_wide_kernel(AttentionArgs P)
 #pragma unroll
       for (int j = 0; j < COLUMNS; j += 2) *reinterpret_cast<v2f *>(to + COLUMNS * c + j) = v2f{o[j], o[j + 1]};
     } else {
-      const float by = l != 0.0f ? 1.0f / l : 0.0f;  // (a row that sees nothing: zeros)
+      const float by = l != 0.0f ? 1.0f / l : none_of;
       const int64_t at = (req.q0 + of) * P.ldo + (int64_t)(head * P.shared + within) * D + COLUMNS * c;
       if constexpr (COLUMNS == 4) {
         store_real4(P.O, at, TYPE, v4f{o[0], o[1], o[2], o[3]} * by);

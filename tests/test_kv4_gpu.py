@@ -664,3 +664,63 @@ def test_queries_of_extreme_size_in_many_rows(gpu, d):
     got, want = c.run(gpu, q, [300], BF16, 0.125), c.exact(q, [300], 0.125)
     assert torch.isfinite(got).all()
     assert float((got - want).abs().max()) <= 2.0 ** -6 * float(want.abs().max())
+
+
+def _positive_keys(lengths, d, page, seed):
+    """A cache whose keys are all positive, from about 1 on."""
+    import torch
+    c = Cached(lengths, 2, d, page, seed=seed)
+    g = torch.Generator().manual_seed(seed + 1)
+    keys = torch.randn(c.keys.shape, generator=g, dtype=torch.float64).abs().cuda() + 1
+    values = torch.randn(c.keys.shape, generator=g, dtype=torch.float64).cuda() + 0.5
+    c.keys, c.values = R.held(keys), R.held(values)
+    assert float(c.keys.min()) > 0.5
+    c.cache = _cache_bytes(keys, values, page)
+    return c
+
+
+@pytest.mark.parametrize("d, queries, keys", [(64, 1, 700), (256, 3, 700), (128, 20, 900), (128, 200, 900), (64, 300, 300), (256, 90, 700)])
+@pytest.mark.parametrize("kind", [BF16, F16])
+def test_a_query_that_is_no_number_against_keys_of_one_sign(gpu, d, queries, keys, kind):
+    """All scores of such a row are minus infinity, or all of them infinity: NaN, unless the row sees no key."""
+    import torch
+    c = _positive_keys([keys, 1, 2], d, 16, seed=23)
+    counts = [queries, 1, 4]  # (the first two of the last request's four come before its two keys)
+    q = torch.randn((queries + 5, 4, d), generator=torch.Generator().manual_seed(25)).to(R.TORCH[kind])
+    blind = torch.zeros((queries + 5, 4), dtype=torch.bool)
+    blind[queries + 1:queries + 3] = True
+    clean = {split: c.run(gpu, q, counts, kind, 0.1, split=split) for split in (True, False)}
+    lost = torch.zeros_like(blind)
+    inf = float("inf")
+    for row, head, channel, x in ((0, 0, 3, -inf), (queries - 1, 1, d - 1, inf), (queries // 2, 2, 0, -inf), (queries, 3, 5, -inf),
+                                  (queries, 0, 5, inf), (queries + 1, 1, 7, -inf), (queries + 2, 0, 7, inf), (queries + 3, 1, 7, -inf),
+                                  (queries + 4, 2, 9, -inf), (queries + 4, 3, 9, inf)):
+        q[row, head, channel] = x
+        lost[row, head] = True
+    if kind == BF16:  # finite, with scores past float32
+        q[queries // 3, 3] = -3e38
+        lost[queries // 3, 3] = True
+    lost &= ~blind
+    for split in (True, False):
+        got = c.run(gpu, q, counts, kind, 0.1, split=split)
+        assert torch.equal(torch.isnan(got).all(-1).cpu(), lost) and torch.equal(torch.isnan(got).any(-1).cpu(), lost), split
+        assert (got[blind] == 0).all()
+        # (the rows that share a wave with them may take their queries unscaled: rounded otherwise, to no fewer bits)
+        fine = ~lost & ~blind
+        assert float((got[fine] - clean[split][fine]).norm() / clean[split][fine].norm()) <= 2.0 ** -7
+
+
+@pytest.mark.parametrize("d, queries", [(64, 1), (128, 40), (128, 200), (256, 90)])
+def test_rows_all_of_whose_pages_are_none(gpu, d, queries):
+    """Such a row sees no key, whatever its length: zeros, also of a query that is no number."""
+    import torch
+    c = Cached([700, 40], 2, d, 32, seed=26)
+    q = torch.randn((queries + 1, 4, d), generator=torch.Generator().manual_seed(27)).to(torch.bfloat16)
+    q[0, 1, 2], q[queries - 1, 2, 3] = float("inf"), float("nan")
+    c.table[0] = -1
+    c.table[0, 5] = c.pages
+    for split in (True, False):
+        got = c.run(gpu, q, [queries, 1], BF16, 0.1, split=split)
+        assert (got[:queries] == 0).all(), split
+        want = c.exact(q[queries:], [0, 1], 0.1)
+        assert float((got[queries:] - want).norm() / want.norm()) <= 2.0 ** -7
