@@ -13,7 +13,8 @@
 //
 // All of it is worked out in float32; where a key's code or a group's step lies so near the middle between two that
 // float32's roundings could decide it, the wave's turn is done again in float64 (one turn in fifty to a hundred): the
-// codes are those of the exact keys, whichever order the squares are summed in.
+// codes are those of the exact keys, whichever order the squares are summed in.  So is a turn, of queries too, with a head whose mean of
+// squares float32 cannot hold, or holds to few bits.
 #include "kv4.h"
 #include "layer_internal.h"
 
@@ -160,6 +161,13 @@ __device__ __forceinline__ float sum_of_head(float x) {
   return x;
 }
 
+// Whether float32 held the mean of squares, eps in it, well whose inverse root this is: from 2^-100 to 2^120.  No square is
+// past it then, and what is lost of small ones is below 2^-40 of the mean.  (As a whole number: one subtraction, one comparison,
+// and NaN is out.)
+__device__ __forceinline__ bool mean_was_held(float root) {
+  return __float_as_uint(root) - ((127u - 60u) << 23) <= (110u << 23);
+}
+
 // EIGHTS: a lane's eight channels meet eight in a row, or are none that are rotated (the number of rotated channels is a
 // multiple of 16, of 8 in pairs); else they are looked for one by one.
 // (five waves to a SIMD where the registers allow it: 67 us with the reading back of the cache, 74 with four)
@@ -216,8 +224,8 @@ __global__ __launch_bounds__(256, EIGHTS && TYPE != REAL_F32 && D < 256 ? 5 : 4)
   };
   float own_by[8], other_by[8];  // of the kind of head that was the last: weights and rotation in one
   int known = -1;
-  uint64_t again = 0, bit = 1;  // the turns (the wave's 64th and all after it: one bit) that are to be done in float64
-  for (int turn = first; turn < turns; turn += step, bit = bit >> 63 ? bit : bit << 1) {
+  uint64_t again = 0, bit = 1;  // the turns (64 at most) that are to be done in float64
+  for (int turn = first; turn < turns; turn += step, bit <<= 1) {
     now = next;
     fetch(turn + step, next);
     const Turned t = of_turn(turn);
@@ -250,6 +258,10 @@ __global__ __launch_bounds__(256, EIGHTS && TYPE != REAL_F32 && D < 256 ? 5 : 4)
         if (t.kind) largest = most3(largest, fabsf(p), fabsf(y[e]));
       }
       const float root = weight ? inverse_root(sum_of_head<LANES>(sum) * (float)(1.0 / D) + P.eps) : 1.0f;
+      if (__any(!mean_was_held(root))) {
+        again |= bit;
+        continue;
+      }
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] *= root;
       if (t.kind == 0) {
@@ -271,27 +283,29 @@ __global__ __launch_bounds__(256, EIGHTS && TYPE != REAL_F32 && D < 256 ? 5 : 4)
   }
   if (!again) return;
   bit = 1;
-  for (int turn = first; turn < turns; turn += step, bit = bit >> 63 ? bit : bit << 1) {
+  for (int turn = first; turn < turns; turn += step, bit <<= 1) {
     const Turned t = of_turn(turn);
-    if (t.kind == 0 || !(again & bit)) continue;
+    if (!(again & bit)) continue;
     fetch(turn, now);
     double z[8];
-    if (t.kind == 1) {
+    if (t.kind < 2) {
+      const float *weight = t.kind ? P.k_weight : P.q_weight;
       join(now);
       double sum = 0.0, root = 1.0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum += (double)now.own[e] * now.own[e];
 #pragma unroll
       for (int d = 1; d < LANES; d *= 2) sum += __shfl_xor(sum, d);
-      if (P.k_weight) root = 1.0 / __builtin_sqrt(sum * (1.0 / D) + (double)P.eps);
-      const Turn by = turn_of<EIGHTS>(P, token, c0, P.k_weight);
+      if (weight) root = 1.0 / __builtin_sqrt(sum * (1.0 / D) + (double)P.eps);
+      const Turn by = turn_of<EIGHTS>(P, token, c0, weight);
       float y[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         z[e] = root * ((double)now.own[e] * by.own[e] * by.cosine[e] + (double)now.other[e] * by.other[e] * by.sine[e]);
         y[e] = (float)z[e];
       }
-      if (P.Ko) write(t, y);
+      if (t.kind == 0 || P.Ko) write(t, y);
+      if (t.kind == 0) continue;
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) z[e] = now.own[e];
@@ -332,8 +346,8 @@ template <typename ARGS>
 hipError_t launch_tokens(void (*const (&kernels)[3][3])(ARGS), ARGS P, int64_t tokens, int head_dim, int type, int groups,
                          hipStream_t s) {
   // a workgroup to a token, which shares what the token is turned by, where there are enough of them (8192 tokens and
-  // their reading back 67 us, 85 with a workgroup to every four turns)
-  P.blocks = tokens >= 8 * compute_units() ? 1 : groups;
+  // their reading back 67 us, 85 with a workgroup to every four turns), and to 64 turns of a wave, which it has a bit for
+  P.blocks = tokens >= 8 * compute_units() ? (groups + 63) / 64 : groups;
   const int64_t most = ((int64_t)1 << 23) / P.blocks > 0 ? ((int64_t)1 << 23) / P.blocks : 1;
   void (*kernel)(ARGS) = kernels[head_dim == 64 ? 0 : (head_dim == 128 ? 1 : 2)][type];
   for (int64_t t = 0; t < tokens; t += most) {

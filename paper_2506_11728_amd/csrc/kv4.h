@@ -49,7 +49,8 @@ __device__ __forceinline__ float kv4_quotient(float num, float s, float r) {
 
 // A lane's eight channels of a group that four neighbouring lanes hold: the word of codes, and the pair of the
 // group (in every lane).  All four lanes call it.  `error`: a bound on what is wrong with a channel.  With one, `unsure` is set
-// where it, or the roundings here, could move a code or the step: there the caller does it again in float64.  Without one, for
+// where it, or the roundings here, could move a code or the step, and where a channel is no number, which may be one that
+// float32 cannot hold before it is cut: there the caller does it again in float64.  Without one, for
 // numbers of 16 bits, it is exact: their quotients by four significant bits are further from the middle between two codes
 // than a rounding, or on it, and whether a step is large enough is asked of products and a difference that are not rounded.
 __device__ __forceinline__ uint32_t kv4_encode(float (&x)[8], float error, uint32_t *pair, bool *unsure) {
@@ -102,7 +103,7 @@ __device__ __forceinline__ uint32_t kv4_encode(float (&x)[8], float error, uint3
   }
   const bool number = none == 0.0f;
   // (of the step: a seventh of twice the error)
-  *unsure = number && error > 0.0f && (off >= 0.5f - error * r * 1.0625f - most * r * 0x1p-21f ||
+  *unsure = error > 0.0f && (!number || off >= 0.5f - error * r * 1.0625f - most * r * 0x1p-21f ||
             (step > 0.0f && fabsf(units - __builtin_rintf(units)) * unit <= error * 0.25f + step * 0x1p-21f));
   const uint16_t half = __builtin_bit_cast(uint16_t, (_Float16)s);  // (exact)
   *pair = number ? (uint32_t)(half >> 7) | ((uint32_t)(int)z & 0xff) << 8 : 0xff;

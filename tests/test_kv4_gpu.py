@@ -228,6 +228,44 @@ def test_queries_alone_beside_a_cache(gpu, d):
     assert torch.equal(out.cpu().reshape(-1, 6, d), want) and (cache == 0xA5).all()
 
 
+@pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("d, rot, style", [(64, 64, 0), (128, 22, 1), (256, 128, 0)])
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-5])
+def test_heads_of_extreme_size(gpu, kind, d, rot, style, eps):
+    """Squares that float32 cannot hold, or holds to few bits, do not reach the result."""
+    import torch
+    t = Heads(gpu, 12, 3, 9, d, kind, 16, rot, seed=31)
+    by = torch.tensor([1e17, 1e18, 1e19, 1e20, 1e30, 2e37, 1e-17, 1e-20, 1e-22, 1e-25, 1e-30, 1e-35], dtype=torch.float64)
+    t.x = (torch.randn(t.x.shape, generator=torch.Generator().manual_seed(32), dtype=torch.float64) * by[:, None]).to(R.TORCH[kind])
+    at = t.positions.long()
+    xq, xk, xv = t.parts()
+    for weights in (True, False):
+        q, _ = t.run(gpu, style, weights=weights, eps=eps)
+        wq = _normed_and_rotated(xq, t.qw if weights else None, eps, t.cos[at], t.sin[at], rot, style)
+        wk = _normed_and_rotated(xk, t.kw if weights else None, eps, t.cos[at], t.sin[at], rot, style)
+        size = wq.abs().amax(-1, keepdim=True) * 2
+        assert _close(q, wq, size, kind, d / 8 + 16), weights
+        kb, vb = t.read(gpu)
+        hk, hv = R.held(wk), R.held(xv.double())
+        assert ((kb.double() - hk).abs() <= R.rounding(hk, kind)).all(), weights
+        assert ((vb.double() - hv).abs() <= R.rounding(hv, kind)).all(), weights
+
+
+@pytest.mark.parametrize("weights", [True, False])
+def test_keys_past_float32_before_they_are_cut(gpu, weights):
+    """A rotation can add two finite channels up to more than float32 holds: such keys are cut, as all others."""
+    import torch
+    t = Heads(gpu, 5, 1, 2, 128, F32, 16, 128, seed=33)
+    t.x[:] = 3e38 * torch.sign(t.x)
+    at = t.positions.long()
+    _, xk, _ = t.parts()
+    t.kw *= 1.5
+    t.run(gpu, 0, weights=weights)
+    hk = R.held(_normed_and_rotated(xk, t.kw if weights else None, 1e-5, t.cos[at], t.sin[at], 128, 0))
+    kb, _ = t.read(gpu)
+    assert torch.isfinite(hk).all() and torch.equal(kb.double(), hk)
+
+
 # ---- attention ----
 
 class Cached:
