@@ -583,9 +583,9 @@ size_t mipgemm_workspace_size_f32(int64_t m, int64_t n, int64_t k,
  *     scales(i) = a(i) / 127, times 1 / sqrt(mean over j of X(i,j)^2 + eps)
  * norm_weight (DEVICE, `cols` float32) makes it an RMS norm and its quantisation in one pass;
  * NULL: no norm, the weights are ones and the factor of the root is left out (`eps` is not
- * used).  z and the scale are formed in float32, the squares are summed in float32, the
- * quotient is correctly rounded, so that Q does not depend on the order of any sum.  A row of
- * zeros gets codes and a scale of zero; a row with an infinity or NaN in z codes of zero and
+ * used).  z and the scale are formed in float32, the squares are summed in float32 (in float64
+ * where it does not hold them well), the quotient is correctly rounded, so that Q does not depend
+ * on the order of any sum.  A row of zeros gets codes and a scale of zero, whatever eps is; a row with an infinity or NaN in z codes of zero and
  * a NaN as its scale, so that what is computed from it is NaN.  X is row-major of x_type with
  * rows ldx elements apart, Q row-major int8 with rows ldq apart; scales holds `rows` float32.
  * Nothing needs more alignment than its type's.  Argument numbers: rows=1 cols=2 X=3 ldx=4

@@ -71,7 +71,8 @@ __device__ __forceinline__ uint32_t four_bytes(uint32_t a, uint32_t b, uint32_t 
 }
 
 // WAVES to a row, ROWS rows to a workgroup; HELD: eights of columns a thread keeps, 0: none.
-template <typename T, int WAVES, int ROWS, int HELD>
+// NORM: through an RMS norm, whose weights are there.
+template <typename T, int WAVES, int ROWS, int HELD, bool NORM>
 __global__ __launch_bounds__(64 * WAVES *ROWS) void quantize_kernel(QuantizeParams P) {
   constexpr int THREADS = 64 * WAVES;
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64 % WAVES, at = threadIdx.x % THREADS;
@@ -81,7 +82,7 @@ __global__ __launch_bounds__(64 * WAVES *ROWS) void quantize_kernel(QuantizePara
   float top = 0.0f, squares = 0.0f, none = 0.0f;  // none: NaN where something is no number
   auto take = [&](int64_t j, float (&v)[8]) {
     load_oct<T>(P, row, j, v);
-    if (P.weight) {
+    if (NORM) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) squares += v[e] * v[e];
       times_weight(P, j, v);
@@ -105,7 +106,7 @@ __global__ __launch_bounds__(64 * WAVES *ROWS) void quantize_kernel(QuantizePara
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
     top = larger(top, __shfl_xor(top, d));
-    squares += __shfl_xor(squares, d);
+    if (NORM) squares += __shfl_xor(squares, d);
   }
   if constexpr (WAVES > 1) {
     __shared__ float both[2][WAVES];
@@ -126,7 +127,8 @@ __global__ __launch_bounds__(64 * WAVES *ROWS) void quantize_kernel(QuantizePara
   const bool finite = top < __builtin_inff();  // (false for a NaN)
   if (at == 0) {
     float scale = finite ? __fdiv_rn(top, 127.0f) : __builtin_nanf("");
-    if (P.weight) scale *= __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(squares, (float)P.cols) + P.eps));
+    if (NORM && top != 0.0f)  // (zero stays zero, whatever eps is)
+      scale *= __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(squares, (float)P.cols) + P.eps));
     P.scales[row] = scale;
   }
   // far from 1, a power of two keeps the reciprocal and the products in range, and changes no quotient
@@ -156,22 +158,38 @@ __global__ __launch_bounds__(64 * WAVES *ROWS) void quantize_kernel(QuantizePara
   } else {
     for (int64_t j = 8 * at; j < P.cols; j += 8 * THREADS) {
       load_oct<T>(P, row, j, x[0]);
-      if (P.weight) times_weight(P, j, x[0]);
+      if (NORM) times_weight(P, j, x[0]);
       put(j, x[0]);
     }
   }
+  // From 2^-100 to 2^120 of the mean no square has passed float32, and what is lost of small ones is below 2^-40 of it.  Elsewhere
+  // the first wave sums them again, in float64, which squares of float32 neither pass nor fall below.
+  if (!NORM || wave != 0 || !finite || top == 0.0f) return;
+  const float mean = squares * __builtin_amdgcn_rcpf((float)P.cols) + P.eps;
+  if (mean >= 0x1p-100f && mean <= 0x1p120f) return;
+  double sum = 0.0;
+  int first = lane;
+  asm volatile("" : "+v"(first));  // (its addresses are not kept over the above)
+#pragma unroll 1
+  for (int64_t j = first; j < P.cols; j += 64) {
+    const double v = load_real(P.X, row * P.ldx + j, real_of<T>::type);
+    sum += v * v;
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+  if (lane == 0) P.scales[row] = (float)((double)top / (127.0 * __builtin_sqrt(sum / (double)P.cols + (double)P.eps)));
 }
 
-template <typename T>
+template <typename T, bool NORM>
 hipError_t launch_for(const QuantizeParams &P, hipStream_t s) {
   void (*kernel)(QuantizeParams);
   unsigned threads = 256;
   int64_t rows = 1;
-  if (P.cols <= 1024) { kernel = quantize_kernel<T, 1, 4, 2>; rows = 4; }
-  else if (P.cols <= 4096) kernel = quantize_kernel<T, 4, 1, 2>;
-  else if (P.cols > 16384) { kernel = quantize_kernel<T, 16, 1, 0>; threads = 1024; }
-  else if (P.rows <= 2 * compute_units()) { kernel = quantize_kernel<T, 16, 1, 2>; threads = 1024; }
-  else kernel = quantize_kernel<T, 4, 1, 8>;
+  if (P.cols <= 1024) { kernel = quantize_kernel<T, 1, 4, 2, NORM>; rows = 4; }
+  else if (P.cols <= 4096) kernel = quantize_kernel<T, 4, 1, 2, NORM>;
+  else if (P.cols > 16384) { kernel = quantize_kernel<T, 16, 1, 0, NORM>; threads = 1024; }
+  else if (P.rows <= 2 * compute_units()) { kernel = quantize_kernel<T, 16, 1, 2, NORM>; threads = 1024; }
+  else kernel = quantize_kernel<T, 4, 1, 8, NORM>;
   const dim3 grid((unsigned)((P.rows + rows - 1) / rows));
   return launch_with(reinterpret_cast<const void *>(kernel), grid, threads, 0, s, &P);
 }
@@ -185,8 +203,9 @@ hipError_t launch_quantize(int64_t rows, int64_t cols, const void *X, int64_t ld
   for (int64_t i = 0; i < rows; i += slab) {
     const QuantizeParams P{static_cast<const uint8_t *>(X) + i * ldx * real_bytes(type), ldx,
                            rows - i < slab ? rows - i : slab, cols, weight, eps, Q + i * ldq, ldq, scales + i};
-    const hipError_t e = type == REAL_F32 ? launch_for<float>(P, s)
-                         : type == REAL_BF16 ? launch_for<__bf16>(P, s) : launch_for<_Float16>(P, s);
+    const hipError_t e = type == REAL_F32    ? (weight ? launch_for<float, true>(P, s) : launch_for<float, false>(P, s))
+                         : type == REAL_BF16 ? (weight ? launch_for<__bf16, true>(P, s) : launch_for<__bf16, false>(P, s))
+                                             : (weight ? launch_for<_Float16, true>(P, s) : launch_for<_Float16, false>(P, s));
     if (e != hipSuccess) return e;
   }
   return hipSuccess;

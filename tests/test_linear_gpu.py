@@ -100,6 +100,30 @@ def test_rows_that_are_no_ordinary_numbers(gpu, cols, norm):
     assert (q[6] == -127).all()
 
 
+@pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("shape", [(14, 100), (14, 3000), (14, 5000), (600, 5000), (14, 20000)])
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-6])
+def test_norms_of_rows_of_extreme_size(gpu, kind, shape, eps):
+    """Squares that float32 cannot hold, or holds to few bits, do not reach the scales."""
+    import torch
+    rows, cols = shape
+    by = torch.tensor([1, 1e17, 1e18, 1e19, 1e20, 1e30, 2e37, 1e-17, 1e-20, 1e-22, 1e-25, 1e-30, 1e-35, 0], dtype=torch.float64)
+    x = torch.randn((rows, cols), generator=torch.Generator().manual_seed(41), dtype=torch.float64)
+    x = (x * by[torch.arange(rows) % 14, None]).to(R.TORCH[kind])
+    w = torch.rand(cols, generator=torch.Generator().manual_seed(42)) + 0.5
+    q, s = _quantize(gpu, x, 1, w, eps)
+    z = x.float().numpy() * w.numpy()
+    a = np.abs(z).max(1)
+    # (a power of two for each row: 127 times the largest would leave float32)
+    want, _ = _codes(z * np.exp2(-np.floor(np.log2(np.where(a > 0, a, 1), dtype=np.float64)))[:, None])
+    assert np.array_equal(q, want)
+    mean = (x.double().numpy() ** 2).mean(1) + float(np.float32(eps))
+    exact = np.where(a > 0, a.astype(np.float64) / 127 / np.sqrt(np.where(a > 0, mean, 1)), 0)
+    # the squares: a chain of at most cols / 64 + 16 float32 additions; a handful of roundings after, of numbers that may be subnormal
+    assert (np.abs(s - exact) <= (cols / 64 + 24) * 2.0 ** -24 * exact + 2.0 ** -149).all()
+    assert (s[13::14] == 0).all()
+
+
 def test_no_columns_and_no_rows(gpu):
     import torch
     s = torch.full((3,), 4.0, device="cuda")
