@@ -213,6 +213,10 @@ __device__ __forceinline__ Request request_of(const AttentionArgs &P, int r) {
 }
 // Of so many keys those that the table can name.
 __device__ __forceinline__ int named_of(const AttentionArgs &P, int keys) { return keys < P.named_kv ? keys : P.named_kv; }
+// Where a range from `begin` on ends, of the tokens that are seen (begin + span can pass 31 bits where max_kv nearly does).
+__device__ __forceinline__ int range_end(const AttentionArgs &P, int begin, int seen) {
+  return P.partials && seen > begin && seen - begin > P.span ? begin + P.span : seen;
+}
 // Where a request's keys and values of one head lie.
 struct Pages {
   typedef const __attribute__((address_space(4))) int32_t *table_ptr;

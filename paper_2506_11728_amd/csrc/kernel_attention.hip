@@ -37,7 +37,7 @@ __global__ __launch_bounds__(64 * WAVES, D <= 128 && RT == 1 ? 4 : (D == 256 && 
   // keys that any row of the tile sees
   const int last_query = (row0 + 16 * RT < rows ? row0 + 16 * RT - 1 : rows - 1) / P.shared;
   const int seen = named_of(P, req.keys - req.queries + last_query + 1);
-  const int end = P.partials ? (seen < begin + P.span ? seen : begin + P.span) : seen;
+  const int end = range_end(P, begin, seen);
   if (range > 0 && begin >= end) return;
 
   v8h q[RT][S::KEY_STEPS];
@@ -261,7 +261,7 @@ __global__ __launch_bounds__(512, 2) void attention_tiles_kernel(AttentionArgs P
   const int before = req.keys - req.queries + 1;  // keys that the first query sees
   auto sees_of = [&](int row) { return before + row / P.shared; };
   const int seen = named_of(P, sees_of(row0 + 16 * RT * W < rows ? row0 + 16 * RT * W - 1 : rows - 1));
-  const int end = P.partials && begin + P.span < seen ? begin + P.span : seen;
+  const int end = range_end(P, begin, seen);
   if (range > 0 && begin >= end) return;
 
   const int wave_row = row0 + wave * (16 * RT);
@@ -525,7 +525,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs P) {
   if (query >= req.queries) return;
   const int seen = named_of(P, req.keys - req.queries + query + 1);
   // (every range that the row's tile went through has written; those that hold none of the row's keys, a sum of zero)
-  const int ranges = seen <= 0 ? 1 : (seen + P.span - 1) / P.span;
+  const int ranges = seen <= 0 ? 1 : (seen - 1) / P.span + 1;
   const float *from = P.partials + ((req.q0 + query) * P.kv_heads * P.shared + head) * (int64_t)P.ranges * PARTIAL<D>;
   float m = LOWEST, l = 0.0f;
   v4f o = {0.0f, 0.0f, 0.0f, 0.0f};

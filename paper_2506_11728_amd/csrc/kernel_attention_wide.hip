@@ -65,7 +65,7 @@ __global__ __launch_bounds__(512, 2) void attention_wide_kernel(AttentionArgs P)
   const int before = req.keys - req.queries + 1;  // keys that the first query sees
   auto sees_of = [&](int row) { return before + row / P.shared; };
   const int seen = named_of(P, sees_of(row0 + ROWS < rows ? row0 + ROWS - 1 : rows - 1));
-  const int end = P.partials && begin + P.span < seen ? begin + P.span : seen;
+  const int end = range_end(P, begin, seen);
   if (range > 0 && begin >= end) return;
 
   // queries: lane's row, channels D / 2 h + 8 i + 0 4 1 5 2 6 3 7 in operand i

@@ -762,3 +762,48 @@ def test_rows_all_of_whose_pages_are_none(gpu, d, queries):
         assert (got[:queries] == 0).all(), split
         want = c.exact(q[queries:], [0, 1], 0.1)
         assert float((got[queries:] - want).norm() / want.norm()) <= 2.0 ** -7
+
+
+@pytest.mark.parametrize("d, queries", [(64, 1), (64, 130)])
+def test_as_many_keys_as_there_can_be(gpu, d, queries):
+    """2^31 - 4097 keys, the most that is not refused: all in one page, but for the last 1023."""
+    import torch
+    page, keys, scale = 1024, 2 ** 31 - 4097, 0.125
+    c = Cached([2 * page], 1, d, page, seed=37, extra=0)
+    first, last = c.rows[0][:page].cuda(), c.rows[0][page:].cuda()
+    # one head's queries take the last page's keys, the other's those of the page before
+    towards = c.keys[last, 0].mean(0) - c.keys[first, 0].mean(0)
+    towards = towards / towards.norm()
+    spread = torch.randn((queries, 2, d), generator=torch.Generator().manual_seed(38), dtype=torch.float64).cuda()
+    spread = spread - (spread @ towards)[..., None] * towards
+    g = torch.randn((2 * page, d), generator=torch.Generator().manual_seed(39), dtype=torch.float64).cuda()
+    near = torch.zeros((2 * page, 1, d), dtype=torch.float64, device="cuda")
+    near[first, 0], near[last, 0] = g[:page] * 0.3, g[page:] * 0.3 + 8 * towards
+    values = c.values.clone()
+    values[last] -= 3
+    c.cache, c.keys, c.values = _cache_bytes(near, values, page), R.held(near), R.held(values)
+    q = spread.clone()
+    q[:, 0] += 50 * towards      # scores near 50: e^50 against 2^31 keys
+    q = q.to(torch.float16)
+    width = (keys + page - 1) // page
+    table = torch.full((1, width), int(first[0]) // page, dtype=torch.int32, device="cuda")
+    table[0, -1] = int(last[0]) // page
+    starts, lengths = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, queries], [keys]))
+    need = gpu.mipgemm_attention_kv4_workspace_size(1, 2, 1, d, queries, keys)
+    assert need > 0
+    ws, out = torch.empty(need, dtype=torch.uint8, device="cuda"), torch.zeros((queries, 2 * d), dtype=torch.float16, device="cuda")
+    gpu.mipgemm_attention_kv4(1, 2, 1, d, F16, q, 2 * d, queries, starts, queries, lengths, keys, c.cache, c.cache.numel(), c.pages,
+                              page, table, width, scale, out, 2 * d, workspace=ws, workspace_bytes=need)
+    out = out.double().reshape(queries, 2, d)
+    at, kept = torch.cat((first, last)), torch.arange(page, device="cuda")
+    for i in (0, queries // 2, queries - 1):
+        here = keys - queries + i + 1 - (width - 1) * page  # keys that the row sees of the last page
+        times = torch.cat((torch.full((page,), float(width - 1), dtype=torch.float64, device="cuda"), (kept < here).double()))
+        for h in range(2):
+            p = torch.softmax(c.keys[at, 0] @ q[i, h].double() * scale + times.log(), 0)
+            want = p @ c.values[at, 0]
+            # two sums of so many additions in float32, each 2^-24 of them at most, p rounded to float16, scores to float32
+            additions = 2 ** 31 // 1024 // 4 // 32 if queries == 1 else 2 ** 31 // 128 // 16
+            bound = (2 * additions * 2.0 ** -24 + 2.0 ** -11 + 2.0 ** -20 * 100) * float(c.values.abs().amax()) + R.rounding(want, F16)
+            assert ((out[i, h] - want).abs() <= bound).all(), (i, h, float((out[i, h] - want).abs().max()))
+        assert float((out[i, 0] - out[i, 1]).norm()) > 1
