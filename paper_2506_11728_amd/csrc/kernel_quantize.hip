@@ -180,6 +180,8 @@ __global__ __launch_bounds__(64 * WAVES *ROWS) void quantize_kernel(QuantizePara
   if (lane == 0) P.scales[row] = (float)((double)top / (127.0 * __builtin_sqrt(sum / (double)P.cols + (double)P.eps)));
 }
 
+constexpr int64_t MOST_THREADS = 1024;  // of a workgroup below, which takes a row or more
+
 template <typename T, bool NORM>
 hipError_t launch_for(const QuantizeParams &P, hipStream_t s) {
   void (*kernel)(QuantizeParams);
@@ -199,7 +201,8 @@ hipError_t launch_for(const QuantizeParams &P, hipStream_t s) {
 hipError_t launch_quantize(int64_t rows, int64_t cols, const void *X, int64_t ldx, int type, const float *weight, float eps,
                            int8_t *Q, int64_t ldq, float *scales, hipStream_t s) {
   // (a grid has at most 2^32 - 1 threads a dimension: taller matrices in slabs)
-  const int64_t slab = (int64_t)1 << 22;
+  constexpr int64_t slab = (int64_t)1 << 21;
+  static_assert(slab * MOST_THREADS < (int64_t)1 << 32, "a row to a workgroup of the most threads");
   for (int64_t i = 0; i < rows; i += slab) {
     const QuantizeParams P{static_cast<const uint8_t *>(X) + i * ldx * real_bytes(type), ldx,
                            rows - i < slab ? rows - i : slab, cols, weight, eps, Q + i * ldq, ldq, scales + i};

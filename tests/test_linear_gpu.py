@@ -124,6 +124,16 @@ def test_norms_of_rows_of_extreme_size(gpu, kind, shape, eps):
     assert (s[13::14] == 0).all()
 
 
+def test_rows_of_more_than_one_launch(gpu):
+    """2^21 rows go into a launch, whose grid then holds them with the most threads a row can have."""
+    import torch
+    rows = 2 ** 21 + 5
+    x = torch.randn((rows, 3), generator=torch.Generator().manual_seed(5))
+    q, s = _quantize(gpu, x, 1, None, 0.0)
+    want, a = _codes(x.numpy())
+    assert np.array_equal(q, want) and np.array_equal(s, a / np.float32(127))
+
+
 def test_no_columns_and_no_rows(gpu):
     import torch
     s = torch.full((3,), 4.0, device="cuda")
