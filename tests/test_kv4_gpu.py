@@ -266,6 +266,25 @@ def test_keys_past_float32_before_they_are_cut(gpu, weights):
     assert torch.isfinite(hk).all() and torch.equal(kb.double(), hk)
 
 
+@pytest.mark.parametrize("d, rot", [(64, 64), (128, 32), (128, 22), (256, 64), (256, 2)])
+@pytest.mark.parametrize("style", [0, 1])
+def test_positions_outside_the_tables(gpu, d, rot, style):
+    """Queries and keys of such a token are NaN in all their channels, rotated or not; its values are as they were."""
+    import torch
+    t = Heads(gpu, 40, 3, 2, d, BF16, 16, rot, seed=35)
+    positions = t.positions.clone()
+    positions[5], positions[6], positions[8] = -1, 500, -2 ** 31
+    lost = torch.zeros(40, dtype=torch.bool)
+    lost[[5, 6, 8]] = True
+    for keys in (False, True):
+        q, k = t.run(gpu, style, positions=positions, keys=keys)
+        assert torch.isnan(q[lost]).all() and torch.isfinite(q[~lost]).all()
+        if keys:
+            assert torch.isnan(k[lost]).all() and torch.isfinite(k[~lost]).all()
+        kb, vb = t.read(gpu)
+        assert torch.isnan(kb[lost]).all() and torch.isfinite(kb[~lost]).all() and torch.isfinite(vb).all()
+
+
 # ---- attention ----
 
 class Cached:
