@@ -285,6 +285,78 @@ def test_positions_outside_the_tables(gpu, d, rot, style):
         assert torch.isnan(kb[lost]).all() and torch.isfinite(kb[~lost]).all() and torch.isfinite(vb).all()
 
 
+def _matrix(gpu, tokens, hq, hkv, d, kind, seed):
+    """Tokens enough for a workgroup each, made on the device."""
+    import torch
+    t = Heads(gpu, 1, hq, hkv, d, kind, 64, d, seed=seed)
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    t.tokens, t.pages = tokens, (tokens + 63) // 64 + 2
+    t.x = (torch.randn((tokens, t.ld), generator=g, device="cuda") * torch.exp(torch.randn((tokens, 1), generator=g, device="cuda"))).to(R.TORCH[kind])
+    t.slots = torch.randperm(t.pages * 64, generator=g, device="cuda")[:tokens]
+    t.positions = torch.randint(0, 500, (tokens,), generator=g, device="cuda", dtype=torch.int32)
+    t.bytes = gpu.mipgemm_kv4_bytes(t.pages, 64, hkv, d)
+    return t
+
+
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+@pytest.mark.parametrize("hq, hkv, d, rot, style", [(37, 9, 128, 128, 0), (70, 21, 64, 64, 1), (13, 5, 256, 96, 0), (9, 40, 128, 22, 0)])
+def test_heads_of_many_tokens(gpu, kind, hq, hkv, d, rot, style):
+    """From 2048 tokens on a wave takes several turns of heads: four and five here, of mixed kinds."""
+    import torch
+    t = _matrix(gpu, 2100, hq, hkv, d, kind, seed=51)
+    t.rot, (t.cos, t.sin) = rot, _tables(500, rot)
+    at = t.positions.long()
+    xq, xk, xv = t.parts()
+    cos, sin = t.cos.cuda()[at], t.sin.cuda()[at]
+    for weights in (True, False):
+        wq = _normed_and_rotated(xq, t.qw.cuda() if weights else None, 1e-5, cos, sin, rot, style)
+        wk = _normed_and_rotated(xk, t.kw.cuda() if weights else None, 1e-5, cos, sin, rot, style)
+        hk, hv = R.held(wk), R.held(xv.double())
+        for keys in (False, True):
+            q, k = t.run(gpu, style, weights=weights, keys=keys)
+            assert _close(q.cuda(), wq, wq.abs().amax(-1, keepdim=True) * 2, kind, d / 8 + 16)
+            assert k is None or _close(k.cuda(), wk, 0, kind, 0)
+            kb, vb = t.read(gpu)
+            assert ((kb.cuda().double() - hk).abs() <= R.rounding(hk, kind)).all()
+            assert ((vb.cuda().double() - hv).abs() <= R.rounding(hv, kind)).all()
+
+
+@pytest.mark.parametrize("hkv", [512, 520])
+def test_as_many_heads_as_a_wave_has_turns(gpu, hkv):
+    """1024 heads of queries and 512 of keys and values are 64 turns of each of four waves; more go to another workgroup."""
+    import torch
+    hq, d = 1024, 64
+    t = _matrix(gpu, 2048, hq, hkv, d, BF16, seed=52)
+    at = t.positions.long()
+    xq, xk, xv = t.parts()
+    wk = _normed_and_rotated(xk, t.kw.cuda(), 1e-5, t.cos.cuda()[at], t.sin.cuda()[at], d, 0)
+    hk, hv = R.held(wk), R.held(xv.double())
+    q, _ = t.run(gpu, 0)
+    wq = _normed_and_rotated(xq, t.qw.cuda(), 1e-5, t.cos.cuda()[at], t.sin.cuda()[at], d, 0)
+    assert _close(q.cuda(), wq, wq.abs().amax(-1, keepdim=True) * 2, BF16, d / 8 + 16)
+    kb, vb = t.read(gpu)
+    assert ((kb.cuda().double() - hk).abs() <= R.rounding(hk, BF16)).all()
+    assert ((vb.cuda().double() - hv).abs() <= R.rounding(hv, BF16)).all()
+
+
+@pytest.mark.parametrize("tokens, hq, hkv, d, style", [(50, 6, 2, 128, 0), (50, 5, 3, 64, 1), (2100, 37, 9, 128, 0), (2100, 13, 5, 256, 1)])
+def test_queries_and_keys_in_place(gpu, tokens, hq, hkv, d, style):
+    import torch
+    t = _matrix(gpu, tokens, hq, hkv, d, BF16, seed=53)
+    # (a head whose squares float32 cannot hold goes through the pass in float64, also in place)
+    t.x[3, :d] *= 1e20
+    t.x[4, hq * d:(hq + 1) * d] *= 1e20
+    q, k = t.run(gpu, style, keys=True)
+    apart = t.cache.clone()
+    x, cache = t.x.clone(), torch.full_like(t.cache, 0xA5)
+    keys = x[:, hq * d:]
+    gpu.mipgemm_qk_norm_rope(tokens, hq, hkv, d, BF16, x, t.ld, keys, t.ld, x[:, (hq + hkv) * d:], t.ld, t.qw.cuda(), t.kw.cuda(), 1e-5,
+                             t.cos.cuda(), t.sin.cuda(), 500, d, style, t.positions, x, t.ld, keys, t.ld, cache, t.bytes, t.pages, 64, t.slots)
+    torch.cuda.synchronize()
+    assert torch.equal(x[:, :hq * d].cpu().reshape(-1, hq, d), q) and torch.equal(x[:, hq * d:(hq + hkv) * d].cpu().reshape(-1, hkv, d), k)
+    assert torch.equal(x[:, (hq + hkv) * d:], t.x[:, (hq + hkv) * d:]) and torch.equal(cache, apart)
+
+
 # ---- attention ----
 
 class Cached:
