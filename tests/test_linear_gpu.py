@@ -124,6 +124,29 @@ def test_norms_of_rows_of_extreme_size(gpu, kind, shape, eps):
     assert (s[13::14] == 0).all()
 
 
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+@pytest.mark.parametrize("shape", [(513, 4097), (600, 11008), (515, 12301), (520, 16384)])
+@pytest.mark.parametrize("norm", [False, True])
+def test_many_rows_of_more_than_4096_columns(gpu, kind, shape, norm):
+    import torch
+    rows, cols = shape
+    x = (torch.randn(shape, generator=torch.Generator().manual_seed(43)) * 3).to(R.TORCH[kind])
+    x[7], x[9, cols - 1], x[11, 0] = 0, float("inf"), float("nan")
+    w = torch.randn(cols, generator=torch.Generator().manual_seed(44)) + 1 if norm else None
+    q, s = _quantize(gpu, x, 5, w, 1e-6)
+    z = x.float().numpy() * (w.numpy() if norm else np.float32(1))
+    lost = np.isin(np.arange(rows), (9, 11))
+    assert np.isnan(s[lost]).all() and (q[lost] == 0).all() and s[7] == 0 and (q[7] == 0).all()
+    want, a = _codes(z[~lost])
+    assert np.array_equal(q[~lost], want)
+    exact = a.astype(np.float64) / 127
+    if norm:
+        exact = exact / np.sqrt((x.double().numpy()[~lost] ** 2).mean(1) + 1e-6)
+    # the squares: a chain of at most cols / 256 + 16 float32 additions; a handful of roundings after
+    bound = ((cols / 256 + 16) * norm + 8) * 2.0 ** -24
+    assert (np.abs(s[~lost] - exact) <= bound * exact).all()
+
+
 def test_rows_of_more_than_one_launch(gpu):
     """2^21 rows go into a launch, whose grid then holds them with the most threads a row can have."""
     import torch
