@@ -240,23 +240,28 @@ struct Pages {
   // the page, or one that is there to be read
   __device__ __forceinline__ const uint8_t *part(int page, bool named) const { return head + (uint64_t)(uint32_t)(named ? page : 0) * bytes; }
   __device__ __forceinline__ int within(int token) const { return token & ((1 << log_page) - 1); }
-  // whether a row sees a key among so many tokens, none of them past the table: one whose page it names
+  // Whether a lane's row sees a key among so many tokens, none of them past the table: one whose page it names.
   __device__ __forceinline__ bool any_named(int tokens) const {
     for (int t = 0; t < tokens; t += 1 << log_page)
       if ((unsigned)table[t >> log_page] < (unsigned)pages) return true;
     return false;
   }
+  // The same asked by a whole wave, 64 pages at a time: the first such token, or 2^31 - 1.
+  __device__ __forceinline__ int first_named(int tokens) const {
+    const int count = tokens > 0 ? ((tokens - 1) >> log_page) + 1 : 0;
+    for (int from = 0; from < count; from += 64) {
+      const int at = from + (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+      const uint64_t found = __ballot(at < count && (unsigned)table[at < count ? at : 0] < (unsigned)pages);
+      if (found) return (from + __builtin_ctzll(found)) << log_page;
+    }
+    return 0x7fffffff;
+  }
 };
 
-// What a row's output is multiplied by, of the sum of its p and the tokens up to its own.  The sum is zero where the row sees no
-// key, whose output is zeros, and where every score is minus infinity, which is also what masks one: those of an infinite query against
-// keys of the other sign, or past float32.  That is no number, and here, once a row, is where the two are told apart.
-__device__ __forceinline__ float of_no_sum(const AttentionArgs &P, const Pages &pages, int tokens) {
-  return pages.any_named(named_of(P, tokens)) ? __builtin_nanf("") : 0.0f;
-}
-__device__ __forceinline__ float inverse_sum(const AttentionArgs &P, const Pages &pages, float sum, int tokens) {
-  return sum != 0.0f ? 1.0f / sum : of_no_sum(P, pages, tokens);
-}
+// What a row's output is multiplied by that has no sum of p.  The sum is zero where the row sees no key, whose output is zeros, and
+// where every score is minus infinity, which is also what masks one: those of an infinite query against keys of the other sign, or
+// past float32.  That is no number, and here, once a row, is where the two are told apart.
+__device__ __forceinline__ float of_no_sum(bool sees_a_key) { return sees_a_key ? __builtin_nanf("") : 0.0f; }
 
 // A range's result for a row in scratch memory: D sums, then base and sum of the softmax.
 template <int D>

@@ -215,7 +215,7 @@ __global__ __launch_bounds__(64 * WAVES, D <= 128 && RT == 1 ? 4 : (D == 256 && 
         *reinterpret_cast<v4f *>(to + part * (D / 16) + i) = v4f{o[i], o[i + 1], o[i + 2], o[i + 3]};
       if (part == 0) *reinterpret_cast<v2f *>(to + D) = v2f{m, l};
     } else {
-      const float by = inverse_sum(P, pages, l, req.keys - req.queries + query + 1);
+      const float by = l != 0.0f ? 1.0f / l : of_no_sum(pages.any_named(named_of(P, req.keys - req.queries + query + 1)));
       const int64_t at = (req.q0 + query) * P.ldo + (int64_t)(head * P.shared + within) * D + part * (D / 16);
 #pragma unroll
       for (int i = 0; i < D / 16; i += 4)
@@ -483,7 +483,7 @@ __global__ __launch_bounds__(512, 2) void attention_tiles_kernel(AttentionArgs P
     float nothing = 0.0f;  // of a row without a sum (lane: row l % 16)
     const v4f l_of = out[t][S::CHANNELS];
     if (!P.partials && __any(l_of[0] == 0.0f || l_of[1] == 0.0f || l_of[2] == 0.0f || l_of[3] == 0.0f))
-      nothing = of_no_sum(P, pages, sees[t]);
+      nothing = of_no_sum(pages.first_named(seen) < sees[t]);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int row = wave_row + 16 * t + 4 * h + e;
@@ -565,9 +565,9 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs P) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], d);
   }
-  if (group != 0) return;
-  const float by = inverse_sum(P, Pages(P, r, 0, 0), l, req.keys - req.queries + query + 1);
-  store_real4(P.O, (req.q0 + query) * P.ldo + (int64_t)head * D + 4 * at, TYPE, o * by);
+  float by = 1.0f / l;
+  if (__any(l == 0.0f)) by = of_no_sum(Pages(P, r, 0, 0).first_named(seen) < seen);  // (the sum is the same in all lanes)
+  if (group == 0) store_real4(P.O, (req.q0 + query) * P.ldo + (int64_t)head * D + 4 * at, TYPE, o * by);
 }
 
 // `count` things, `each` workgroups to one, as many in a launch as a grid holds.

@@ -472,7 +472,7 @@ __global__ __launch_bounds__(512, 2) void attention_wide_kernel(AttentionArgs P)
   bool no_sum = false;
 #pragma unroll
   for (int v = 0; v < 16; ++v) no_sum = no_sum || out[COLUMNS][v] == 0.0f;
-  if (!P.partials && __any(no_sum)) nothing = of_no_sum(P, pages, sees);
+  if (!P.partials && __any(no_sum)) nothing = of_no_sum(pages.first_named(seen) < sees);
 #pragma unroll
   for (int v = 0; v < 16; ++v) {
     const int row_in = 8 * (v / 4) + 4 * h + v % 4, at_row = wave_row + row_in;

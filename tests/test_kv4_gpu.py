@@ -795,6 +795,22 @@ def test_queries_of_extreme_size_in_many_rows(gpu, d):
     assert float((got - want).abs().max()) <= 2.0 ** -6 * float(want.abs().max())
 
 
+@pytest.mark.parametrize("d, queries", [(64, 1), (128, 40), (128, 200), (256, 90)])
+def test_lengths_past_a_table_that_names_no_page(gpu, d, queries):
+    """Rows whose length is beyond what the table can name, of which it names nothing: zeros."""
+    import torch
+    c = Cached([700, 40], 2, d, 16, seed=28)
+    q = torch.randn((queries + 1, 4, d), generator=torch.Generator().manual_seed(29)).to(torch.bfloat16)
+    c.table[0] = -1
+    assert c.table.shape[1] * 16 == 704
+    c.lengths[0] = 5000
+    for split in (True, False):
+        got = c.run(gpu, q, [queries, 1], BF16, 0.1, split=split)
+        assert (got[:queries] == 0).all(), split
+        want = c.exact(q[queries:], [0, 1], 0.1)
+        assert float((got[queries:] - want).norm() / want.norm()) <= 2.0 ** -7
+
+
 def _positive_keys(lengths, d, page, seed):
     """A cache whose keys are all positive, from about 1 on."""
     import torch
