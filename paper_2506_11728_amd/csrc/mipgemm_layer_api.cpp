@@ -187,7 +187,7 @@ int mipgemm_attention_kv4(int64_t requests, int64_t q_heads, int64_t kv_heads, i
   const int64_t named = P.table_stride << P.log_page;
   P.named_kv = named < P.max_kv ? (int)named : P.max_kv;
   P.ranges = 1; P.span = 0; P.first = 0;
-  P.scale = scale;
+  P.scale = scale < 2.3e38f ? scale : 2.3e38f;  // (the kernels multiply it by log2 e: not to infinity, which makes NaN of zero)
   return static_cast<int>(mip::launch_attention(P, (int)requests, (int)head_dim, type, workspace, workspace_bytes,
                                                 static_cast<hipStream_t>(stream)));
 }

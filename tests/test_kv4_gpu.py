@@ -544,6 +544,21 @@ def test_queries_of_extreme_size(gpu):
         assert float((got - want).abs().max()) <= 2.0 ** -6 * float(want.abs().max())
 
 
+@pytest.mark.parametrize("d, queries", [(64, 1), (128, 40), (128, 200), (256, 90)])
+@pytest.mark.parametrize("kind", [BF16, F16])
+def test_scales_at_both_ends(gpu, d, queries, kind):
+    """Queries of zeros weigh all keys alike, whatever the scale; so does every query at the smallest."""
+    import torch
+    c = Cached([300], 2, d, 16, seed=45)
+    q = torch.zeros((queries, 4, d))
+    want = c.exact(q, [queries], 1.0)
+    for scale in (3.4e38, 1e-45, 1e-38):
+        got = c.run(gpu, q, [queries], kind, scale)
+        assert float((got - want).norm() / want.norm()) <= 2.0 ** -8, scale
+    got = c.run(gpu, q + 1, [queries], kind, 1e-45)
+    assert float((got - want).norm() / want.norm()) <= 2.0 ** -8
+
+
 def test_no_number_among_queries_stays_in_its_row(gpu):
     import torch
     c = Cached([300, 90], 2, 128, 16)
