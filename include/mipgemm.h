@@ -704,8 +704,8 @@ int mipgemm_kv4_read(int64_t tokens, int64_t kv_heads, int64_t head_dim, int typ
  * h / (q_heads / kv_heads).  type is that of Q and O: MIPGEMM_BF16 or MIPGEMM_F16; rows of Q and O hold
  * all heads, ldq and ldo elements apart, and O must not overlap Q.  scale is positive.
  * Scores, softmax and sums are float32; p is rounded to float16 for the product with
- * the values, and bfloat16 queries, where a key head has more than 128 rows of them, to
- * float16 with the scale in them.  A key, a query or a group of a value that is no number makes
+ * the values, and bfloat16 queries of 64 or 128 channels, where a key head has more than 128 rows of
+ * them, to float16 with the scale in them.  A key, a query or a group of a value that is no number makes
  * NaN what sees it (of a value, the 32 channels of the group) and nothing else; so do scores all of which
  * float32 cannot hold.
  *
@@ -713,7 +713,10 @@ int mipgemm_kv4_read(int64_t tokens, int64_t kv_heads, int64_t head_dim, int typ
  * and max_kv are the host's upper bounds: what the arrays say beyond them is cut to them, and
  * keys whose page the table does not name (beyond table_stride, or a number outside 0 .. pages - 1)
  * are not seen.  So a call with bounds that stay the same can be captured in a graph and
- * replayed over growing lengths.  Rows of O that belong to no request are not written.
+ * replayed over growing lengths.  Rows of O that belong to no request are not written.  The bounds
+ * also say how the call is cut, for all of its requests alike: single tokens over long caches take
+ * several times longer beside a prompt than in a call of their own, and bounds far above the lengths
+ * cost some of the time that close ones save.
  *
  * `workspace` is optional: with mipgemm_attention_kv4_workspace_size bytes (16 bytes more
  * serve where it is not 16-byte aligned), or those for q_rows rows where they are fewer, calls with few

@@ -4,13 +4,16 @@
 // in one pass over the keys, with the running maximum and sum of the softmax in float32.  The queries of
 // all heads that share a key head are the rows of one product: row = query * shared + head.
 //
-// The products are v_mfma_f32_16x16x32_f16 on the cache's own numbers: a code's nibble under the exponent of
+// The products are float16 matrix instructions on the cache's own numbers: a code's nibble under the exponent of
 // 1024 or of 64 is the float16 1024 + n (64 + n), the zero point is subtracted and the step multiplied in float16,
-// and both are exact.  Queries in bfloat16 are multiplied by a power of two that brings the row's largest
-// below 32768 and are exact as float16 wherever they are not 2^-24 times smaller than that; the power is
-// taken back in the scale of the scores.  What is rounded is p: to float16, eleven bits, less than the output's
-// own rounding in bfloat16.  Its sum, one more column of the product with the values, is of
-// the rounded p.
+// and both are exact.  What is rounded is p: to float16, eleven bits, which is what the instruction takes beside the values.  That is
+// an eighth of the output's own rounding in bfloat16 and as much as it in float16 (one query of 301 keys: 2.7e-4 of the result
+// instead of 2.0e-4).  Its sum, one more column of the product with the values, is of the rounded p.
+//
+// Of the kernels for few rows and for 256 channels, which are what follows here (kernel_attention_wide.hip has its own form
+// of it): the instructions are v_mfma_f32_16x16x32_f16.  Queries in bfloat16 are multiplied by a power of two that
+// brings the row's largest below 32768 and are exact as float16 wherever they are not 2^-24 times smaller than that;
+// the power is taken back in the scale of the scores.
 //
 // Operand layout of the instruction: lane l gives row (column) l % 16, eight k from 8 (l / 16) on; the result has
 // column l % 16 and rows 4 (l / 16) .. + 3.  Any order of k will do that both operands share.

@@ -467,6 +467,7 @@ static const TileForm kTileForms[] = {
      0.197, 0.198, 0.0685, 0.0555, -0.161, -0.039, 0.944, 0.0514},
 };
 
+// (A linear layer's write-back is taken for that of floats: its residual, and what C takes less in 16 bits, are not in the fit.)
 static double predicted_us(const TileForm &f, const Problem &p, int64_t cus) {
   const int64_t tiles = ((p.m + f.bm - 1) / f.bm) * ((p.n + f.bn - 1) / f.bn);
   const int64_t full = tiles / (f.per_cu * cus), rest = (tiles % (f.per_cu * cus) + cus - 1) / cus;

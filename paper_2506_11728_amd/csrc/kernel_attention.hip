@@ -1,10 +1,11 @@
 // Attention over the 4-bit cache: the kernel for few rows (single tokens and drafted ones), the one for many
 // (prompts and their chunks), and the one that joins ranges of keys.
 //
-// Few rows: bound by the cache's bytes where there are enough keys (one query of 32 heads over 131001 keys of 8: 31 us, 151 MB
-// at 4.9 TB/s, which is the rate of a copy; joining its 128 ranges 4.8 more), by the vector instructions that make float16 of
-// the codes where rows have to share them unevenly (32 requests of 174 to 8192 keys 39 us, 4.0 TB/s), and by first loads and
-// last sums in short calls (301 keys 6.2 us).  A workgroup takes the rows of one request and key head (16 or 32 of them; more rows,
+// Few rows: bound by the cache's bytes where there are enough keys (one query of 32 heads over 131001 keys of 8: 34 us from memory,
+// 151 MB at 4.4 TB/s, and 31 where they lie in the last-level cache; joining its 128 ranges 4.3 more), by unequal requests where
+// those differ (32 of 174 to 8192 keys, 3 % more bytes: 42 us; the vector instructions that make float16 of the codes are
+// 20 us of issue in either), and by first loads and last sums in short calls (301 keys 6.0 us).  Ranges are cut by the bound
+// max_kv and rows by max_q: 4096 keys take 9.6 us under a bound of 4096 and 15 under one of 131072.  A workgroup takes the rows of one request and key head (16 or 32 of them; more rows,
 // more workgroups, which find the codes in L2) and a range of its keys; its four waves take steps of 32 keys in turn, each with a
 // running maximum, sum and output of its own, which meet in LDS at the end.  Where requests and heads are too few to
 // occupy the device the keys are cut into ranges, and a second, small kernel joins them.
@@ -231,7 +232,7 @@ __global__ __launch_bounds__(64 * WAVES, D <= 128 && RT == 1 ? 4 : (D == 256 && 
 // A SIMD has two waves, one of either half of the workgroup, and the halves run half a tile apart, held there by a
 // barrier after every half: while one wave keeps the matrix unit busy (output of a tile, scores of the next), the other
 // has the vector unit to itself (weights of a tile, its share of the codes to come).  Side by side they take the
-// two units in turns.  2048 queries of 16 heads over 4096 keys of 4: 188 us, 550 TFLOP/s.
+// two units in turns.  2048 queries of 16 heads over 4096 keys of 4: 177 us, 580 TFLOP/s.
 template <int TYPE>
 __global__ __launch_bounds__(512, 2) void attention_tiles_kernel(AttentionArgs P) {
   constexpr int D = 256;

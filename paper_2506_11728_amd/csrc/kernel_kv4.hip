@@ -4,8 +4,9 @@
 //
 // Every number is read once and written once, in one launch, so that nothing between the projection and the cache
 // goes to memory: 8192 tokens of 32 heads of queries and 8 of keys and values, 128 channels in bfloat16, would take
-// 34 us at the rate of a copy.  They take 54 (177 MB at 3.3 TB/s), bound by vector instructions: some 260 for a
-// wave's heads, which keep the SIMDs busy three quarters of the time.  d / 8 lanes to a head, eight channels to a lane:
+// 34 us at the rate of a copy.  They take 54 resident, bound by vector instructions (some 260 for a wave's heads, 41 us of
+// issue), and 70 from memory (177 MB at 2.5 TB/s), where a wave waits for its numbers besides.  In float32 93, with rotations that
+// are no multiple of 16 133, with keys as numbers, all of which go through float64, 82.  d / 8 lanes to a head, eight channels to a lane:
 // a wave takes 8, 4 or 2 heads at a time, all of one kind, so that what kind they are is decided by scalar branches.
 // What a rotation joins to a lane's channels is loaded a second time (from the first cache) rather than passed between
 // lanes: through LDS the kernel took 88 us.  Weights and rotation become one factor for each channel and one for its

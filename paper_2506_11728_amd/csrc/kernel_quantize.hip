@@ -7,9 +7,12 @@
 // Bound by memory: x is read once, a byte an element written.  A row stays in the registers of its workgroup
 // between the reduction and the rounding where it fits (16384 numbers); longer rows are read a second time,
 // through the cache.  A wave to a row up to 1024 columns, four waves up to 4096; up to 16384 sixteen waves
-// where there is a workgroup of them at a time for every row (48 rows of 11008: 4.2 us against 6.8 with four), else four.
-// 4096 rows of 4096 in bfloat16 with a norm: 14.6 us, 50 MB at 3.4 TB/s, a dozen vector instructions to a number; a row of
-// 4096: 3.0 us, of which some 2 are the launch.
+// where there is a workgroup of them at a time for every row (48 rows of 11008: 3.7 us against 6.8 with four), else four.
+// 4096 rows of 4096 in bfloat16 with a norm: 14.4 us from memory (50 MB at 3.5 TB/s), 13 resident, 11 without a norm.  21 vector
+// instructions to a number are 9 us of issue, and two rounds of workgroups, each of which loads, meets at a barrier and
+// stores, do not overlap with it altogether (8192 rows 25 us, 16384 44).  4096 rows of 11008, 64 numbers to a thread and so
+// four workgroups to a compute unit: 41 us from memory (3.3 TB/s), 39 resident, 30 without a norm.  A row of 4096: 2.5 us, of
+// which some 2 are the launch.
 #include "layer_internal.h"
 #include "real.h"
 

@@ -20,6 +20,10 @@ constexpr int LINEAR_OUT = 5;  // the kernels' UNS parameter: both operands sign
 //   0: max(y, floor), floor 0 or -infinity
 //   1: y / (1 + exp(-y (c1 + c3 y^2))): SiLU, and GELU's tanh form, since (1 + tanh u) / 2 = 1 / (1 + exp(-2 u))
 //   2: y * erfc(-y / sqrt 2) / 2: GELU
+// The argument of the exponential is one rounded product (of two, GELU's), |t| 2^-24 off at most, and so is the exponential,
+// relatively: where y is far below zero and the result as small, 20 2^-24 of it at y = -20.  In 16 bits that does not show, in float32
+// it is the last few bits of a tail of 1e-8; a second product for what the first one's rounding loses would be five
+// instructions more in a write-back that nothing overlaps.
 template <int KIND>
 struct Activate {
   float c1, c3;  // kind 0: the floor in c1
