@@ -736,6 +736,116 @@ int mipgemm_attention_kv4(int64_t requests, int64_t q_heads, int64_t kv_heads, i
                           void *O, int64_t ldo,
                           void *workspace, size_t workspace_bytes, void *stream);
 
+/* scores of mipgemm_route */
+#define MIPGEMM_SOFTMAX 0 /* exp(l(e)) / sum over all experts of exp(l) */
+#define MIPGEMM_SIGMOID 1 /* 1 / (1 + exp(-l(e))) */
+
+/*
+ * Routing of tokens to experts, and the tokens' rows sorted by expert.  For each token with
+ * logits l(e) of `experts` experts
+ *     s(e) = its scores (scoring: MIPGEMM_SOFTMAX or MIPGEMM_SIGMOID),  c(e) = s(e) + bias(e)
+ * (bias: DEVICE, `experts` float32, or NULL: 0; it chooses and does not weigh).  The experts are
+ * `groups` groups of as many neighbours each; a group's score is the sum of its group_best (1 or
+ * 2) largest c, and the top_groups groups of the largest scores stay.  ids(token, 0 .. top - 1)
+ * are the experts with the largest c in them, the largest first,
+ *     weights(token, j) = scale s(ids(j)) [ / the sum over j of s(ids(j)), with `normalise` ].
+ * Of equal ones, groups or experts, the lowest index comes first.  What is compared are the exact c
+ * (where float32 leaves a comparison in doubt it is made in float64), so that a choice does not
+ * depend on the order of a sum; weights are within a few roundings of float32.  An expert whose logit or bias is
+ * -infinity is never chosen and adds nothing to a group; places that are left over get an id of -1
+ * and a weight of 0.  A token with a NaN among its c (as +infinity makes it under softmax)
+ * gets ids of -1 and NaN as its weights, so that what is computed from it is NaN.
+ *
+ * starts, order and places (int32, DEVICE) are those rows by expert: assignment t top + j is row
+ * places(t top + j) of them (-1 if it has no expert), order(row) = t top + j, expert e has the
+ * rows starts(e) .. starts(e + 1) - 1 (experts + 1 entries), in the order of their tokens; order is not
+ * written from starts(experts) on.  starts NULL: the rows are not sorted, order and places are
+ * not used; order or places NULL: not written.
+ *
+ * logits are of `type`, tokens ldl elements apart; ids, weights and places hold `top` entries to a token.
+ * With starts and more than 32 tokens, a workspace of
+ * mipgemm_route_workspace_size bytes (16-byte aligned) is needed.  Argument numbers: tokens=1 (at most 2^26)
+ * experts=2 (1 to 1024) top=3 (1 to 32) logits=4 ldl=5 type=6 bias=7 scoring=8 groups=9 (1 to 64, a
+ * divisor of experts) top_groups=10 group_best=11 (no more than a group has) normalise=12 scale=13
+ * (finite) ids=14 weights=15 starts=16 order=17 places=18 workspace=19 workspace_bytes=20
+ * stream=21.  top is at most what top_groups groups hold (else -3), and tokens * top below 2^31 (else -1).
+ */
+size_t mipgemm_route_workspace_size(int64_t tokens, int64_t experts, int64_t top);
+int mipgemm_route(int64_t tokens, int64_t experts, int64_t top,
+                  const void *logits, int64_t ldl, int type,
+                  const float *bias, int scoring,
+                  int64_t groups, int64_t top_groups, int64_t group_best,
+                  int normalise, float scale,
+                  int32_t *ids, float *weights,
+                  int32_t *starts, int32_t *order, int32_t *places,
+                  void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The linear layers of experts on 8-bit operands: rows sorted by expert, each multiplied by the
+ * weights of its own.  Row p of expert e (starts(e) <= p < starts(e + 1); starts as mipgemm_route
+ * gives it, read on the device alone) is
+ *     y(p,j) = float(S(p,j)) a_scales(i) b_scales(e,j) + bias(e,j),   S = A(i) . B(e,j)
+ *     C(p,j) = act(y(p,j)),   or with `gated` act(y(p,j)) y(p,n+j)
+ * with i = order(p) / top, rounded down (order NULL: i = p), so that tokens are read where they
+ * are.  S is the int32 sum (wrapping modulo 2^32), what is behind it as in mipgemm_s8s8_linear, rounded once to the
+ * type of C.  An expert has n columns of weights, with `gated` 2 n: B holds for each a row of k
+ * bytes, rows ldb apart and experts strideB; b_scales and bias hold as many float32 to an
+ * expert, one expert behind the other.  a_scales (a_rows float32), b_scales and bias may each be NULL: 1, 1 and 0.
+ *
+ * `rows` is the host's bound on the rows (tokens * top): starts beyond it are cut to it.  Rows of C
+ * behind starts(experts) are not written.  An i outside 0 .. a_rows - 1 reads a row of zeros.  So a
+ * call with the same bound can be captured in a graph and replayed over other routings.
+ * C must not overlap what is read.  Operands with 16-byte aligned rows (lda, ldb, strideB multiples of 16) are streamed;
+ * others are read as they are, more slowly.
+ * Argument numbers: rows=1 experts=2 (1 to 1024) n=3 k=4 A=5 lda=6 a_rows=7 (at least 1, or with order NULL at
+ * least rows) a_scales=8 starts=9 order=10 top=11 B=12 ldb=13 strideB=14 (at least the rows of an expert
+ * times ldb, where there is more than one) b_scales=15 bias=16 activation=17 gated=18 C=19 ldc=20 c_type=21 stream=22.
+ */
+int mipgemm_s8s8_experts(int64_t rows, int64_t experts, int64_t n, int64_t k,
+                         const int8_t *A, int64_t lda, int64_t a_rows, const float *a_scales,
+                         const int32_t *starts, const int32_t *order, int64_t top,
+                         const int8_t *B, int64_t ldb, int64_t strideB,
+                         const float *b_scales, const float *bias,
+                         int activation, int gated,
+                         void *C, int64_t ldc, int c_type, void *stream);
+
+/* norms of mipgemm_join_rows */
+#define MIPGEMM_NO_NORM 0
+#define MIPGEMM_RMS_NORM 1   /* v weight / sqrt(mean of v^2 + eps) + bias */
+#define MIPGEMM_LAYER_NORM 2 /* (v - mean of v) weight / sqrt(mean of (v - mean)^2 + eps) + bias */
+
+/*
+ * The end of a block and the beginning of the next, in one pass over the rows:
+ *     y(i) = sum over j < parts of weights(i,j) X(places(i,j)),   u = post_norm(y)
+ *     H(i) = R(i) + scale gate(i) u(i)                            the residual stream
+ *     z(i) = norm(H(i)),   N(i) = z(i),   Q(i) = rint(127 z(i) / a(i)), scales(i) = a(i) / 127
+ * with a(i) the largest |z(i)|.  X has x_rows rows; places (rows x parts int32, as mipgemm_route gives
+ * them) NULL: i parts + j; weights (rows x parts float32) NULL: ones.  A place outside 0 ..
+ * x_rows - 1 stands for a row of zeros.  gate: one row to gate_rows neighbouring rows, ldg elements apart (a
+ * sequence's gate; gate_rows >= rows: the same for all); NULL: ones.  R NULL: zeros.  H, N, and Q with scales may each be
+ * NULL: not written.  H may be R, with the same leading dimension; otherwise what is written must
+ * not overlap what is read.  X, gate, R, H and N are of `type`; norms' weights and biases hold `cols` float32,
+ * NULL: ones and zeros; without a norm they are not used.
+ * Everything is in float32 or better (sums of squares that float32 does not hold in float64) with one
+ * rounding to each result; H is rounded before it is normed: N and Q are of the stream as it is
+ * stored.  Under MIPGEMM_RMS_NORM without a bias, Q and scales are those of mipgemm_quantize_rows on H, the codes bit for
+ * bit: a row of zeros has codes and a scale of zero; a row with an infinity or NaN in z codes of zero and
+ * NaN as its scale.  A row of zeros (LAYER_NORM: of equal numbers) is normed to zeros, whatever eps is, plus the bias.
+ * Argument numbers: rows=1 cols=2 (at most 16384) parts=3 (1 to 1024) type=4 X=5 ldx=6 x_rows=7
+ * (with places NULL at least rows * parts) places=8 weights=9 post_norm=10 post_weight=11
+ * post_bias=12 gate=13 ldg=14 gate_rows=15 (at least 1) scale=16 (finite) R=17 ldr=18 H=19 ldh=20 norm=21 norm_weight=22
+ * norm_bias=23 eps=24 (finite, not negative) N=25 ldn=26 Q=27 ldq=28 scales=29 stream=30.
+ */
+int mipgemm_join_rows(int64_t rows, int64_t cols, int64_t parts, int type,
+                      const void *X, int64_t ldx, int64_t x_rows,
+                      const int32_t *places, const float *weights,
+                      int post_norm, const float *post_weight, const float *post_bias,
+                      const void *gate, int64_t ldg, int64_t gate_rows, float scale,
+                      const void *R, int64_t ldr, void *H, int64_t ldh,
+                      int norm, const float *norm_weight, const float *norm_bias, float eps,
+                      void *N, int64_t ldn, int8_t *Q, int64_t ldq, float *scales,
+                      void *stream);
+
 /*
  * Static, human-readable text for a return value of the functions above.  For a
  * negative code the text gives the argument number and, in parentheses, the name

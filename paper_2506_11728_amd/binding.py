@@ -21,6 +21,9 @@ OVERWRITE, ACCUMULATE = 0, 1
 F32, BF16, F16 = 0, 1, 2
 NONE, RELU, GELU, GELU_TANH, SILU = 0, 1, 2, 3, 4
 ROTATE_HALVES, ROTATE_PAIRS = 0, 1
+# scores of a router, norms of a block's ends
+SOFTMAX, SIGMOID = 0, 1
+NO_NORM, RMS_NORM, LAYER_NORM = 0, 1, 2
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libmipgemm.so")
@@ -62,7 +65,8 @@ def exported_symbols():
             "mipgemm_conv_s8u8s32_with_sums", "mipgemm_conv_s8u8f32_with_sums", "mipgemm_conv_s8u8s8",
             "mipgemm_s16s16s32", "mipgemm_workspace_size_s16",
             "mipgemm_quantize_rows", "mipgemm_s8s8_linear", "mipgemm_kv4_bytes", "mipgemm_qk_norm_rope",
-            "mipgemm_kv4_read", "mipgemm_attention_kv4", "mipgemm_attention_kv4_workspace_size"]
+            "mipgemm_kv4_read", "mipgemm_attention_kv4", "mipgemm_attention_kv4_workspace_size",
+            "mipgemm_route", "mipgemm_route_workspace_size", "mipgemm_s8s8_experts", "mipgemm_join_rows"]
 
 
 def load_library() -> ctypes.CDLL:
@@ -164,7 +168,8 @@ def load_library() -> ctypes.CDLL:
                 fn = getattr(lib, name)
                 fn.restype = ctypes.c_int
                 fn.argtypes = [_CTYPES[f] for f in _LAYER_FORMATS[name]]
-            for name, count in (("mipgemm_kv4_bytes", 4), ("mipgemm_attention_kv4_workspace_size", 6)):
+            for name, count in (("mipgemm_kv4_bytes", 4), ("mipgemm_attention_kv4_workspace_size", 6),
+                                ("mipgemm_route_workspace_size", 3)):
                 fn = getattr(lib, name)
                 fn.restype = ctypes.c_size_t
                 fn.argtypes = [i64] * count
@@ -186,6 +191,8 @@ _LAYER_FORMATS = {
     "mipgemm_quantize_rows": "qqpqipfpqps", "mipgemm_s8s8_linear": "qqqpqppqippipqpqipzs",
     "mipgemm_qk_norm_rope": "qqqqipqpqpqppfppqqippqpqpzqqps", "mipgemm_kv4_read": "qqqipzqqppqpqs",
     "mipgemm_attention_kv4": "qqqqipqqpqpqpzqqpqfpqpzs",
+    "mipgemm_route": "qqqpqipiqqqifppppppzs", "mipgemm_s8s8_experts": "qqqqpqqpppqpqqppiipqis",
+    "mipgemm_join_rows": "qqqipqqppipppqqfpqpqippfpqpqps",
 }
 _CTYPES = {"q": ctypes.c_int64, "i": ctypes.c_int, "p": ctypes.c_void_p, "z": ctypes.c_size_t, "s": ctypes.c_void_p,
            "f": ctypes.c_float}
@@ -622,6 +629,36 @@ def mipgemm_attention_kv4(requests, q_heads, kv_heads, head_dim, type, Q, ldq, q
     return _run(check, "mipgemm_attention_kv4", requests, q_heads, kv_heads, head_dim, type, Q, ldq, q_rows, q_starts, max_q,
                 kv_lengths, max_kv, cache, cache_bytes, pages, page_tokens, block_table, table_stride, scale, O, ldo,
                 workspace, workspace_bytes, stream)
+
+
+# ---- a mixture of experts ----
+
+def mipgemm_route_workspace_size(tokens, experts, top) -> int:
+    return int(load_library().mipgemm_route_workspace_size(tokens, experts, top))
+
+
+def mipgemm_route(tokens, experts, top, logits, ldl, type, bias, scoring, groups, top_groups, group_best, normalise, scale,
+                  ids, weights, starts=None, order=None, places=None, workspace=None, workspace_bytes=0, stream=None, check=True):
+    """ids (int32), weights (float32): each token's experts; starts, order, places: the tokens' rows sorted by expert (see
+    include/mipgemm.h)."""
+    return _run(check, "mipgemm_route", tokens, experts, top, logits, ldl, type, bias, scoring, groups, top_groups, group_best,
+                normalise, scale, ids, weights, starts, order, places, workspace, workspace_bytes, stream)
+
+
+def mipgemm_s8s8_experts(rows, experts, n, k, A, lda, a_rows, a_scales, starts, order, top, B, ldb, strideB, b_scales, bias,
+                         activation, gated, C, ldc, c_type, stream=None, check=True):
+    """C = act(a_scales * (A * B) * b_scales + bias) for rows sorted by expert, each on its own expert's int8 weights."""
+    return _run(check, "mipgemm_s8s8_experts", rows, experts, n, k, A, lda, a_rows, a_scales, starts, order, top, B, ldb, strideB,
+                b_scales, bias, activation, gated, C, ldc, c_type, stream)
+
+
+def mipgemm_join_rows(rows, cols, parts, type, X, ldx, x_rows, places, weights, post_norm, post_weight, post_bias, gate, ldg,
+                      gate_rows, scale, R, ldr, H, ldh, norm, norm_weight, norm_bias, eps, N, ldn, Q=None, ldq=None, scales=None,
+                      stream=None, check=True):
+    """H = R + scale * gate * post_norm(sum of weighted rows of X); N and Q (int8, with scales): norm(H) (see include/mipgemm.h)."""
+    return _run(check, "mipgemm_join_rows", rows, cols, parts, type, X, ldx, x_rows, places, weights, post_norm, post_weight,
+                post_bias, gate, ldg, gate_rows, scale, R, ldr, H, ldh, norm, norm_weight, norm_bias, eps, N, ldn, Q,
+                cols if ldq is None else ldq, scales, stream)
 
 
 ERR_STATIC_SCRATCH = -100

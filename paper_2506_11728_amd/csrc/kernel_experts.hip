@@ -1,0 +1,137 @@
+// The experts' products of rows sorted by expert, for operands of any alignment and any k:
+//     C(p, j) = act(float(A(p) . B(e, j)) a_scale b_scale + bias)
+// 64 rows of one expert by 64 columns to a workgroup (with a gate 64 pairs of columns), k in blocks of 64 through registers
+// into LDS, two stages, v_mfma_i32_32x32x32_i8.
+#include "experts.h"
+#include "dma_common.h"
+
+namespace mip {
+
+namespace {
+
+constexpr int TM = 64, TN = 64, TK = 64;
+
+struct Params {
+  ExpertsArgs X;
+  int64_t slot0, column0;
+};
+
+template <int GATED>
+__global__ __launch_bounds__(256) void experts_kernel(Params P) {
+  constexpr int BROWS = TN * (1 + GATED), STAGE = (TM + BROWS) * TK;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * STAGE];
+  __shared__ float scales[TM];
+  const ExpertsArgs &X = P.X;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const ExpertTile tile = expert_tile(X.starts, X.experts, X.rows, TM, P.slot0 + blockIdx.y, lane);
+  if (tile.count == 0) return;
+  const int64_t n0 = P.column0 + (int64_t)blockIdx.x * TN;
+  const int64_t outputs = GATED ? 2 * X.n : X.n;
+  using SA = Stage<TM, true, TK>;
+  using SB = Stage<BROWS, true, TK>;
+  // this thread's pieces: one of A, one or two of B
+  const uint8_t *from[SA::PER_THREAD + SB::PER_THREAD];
+  int to[SA::PER_THREAD + SB::PER_THREAD], deep[SA::PER_THREAD + SB::PER_THREAD];
+#pragma unroll
+  for (int i = 0; i < SA::PER_THREAD; ++i) {
+    int a, c;
+    SA::chunk_of(i, tid, a, c);
+    const ExpertRow r = expert_row(X, tile.first + (a < tile.count ? a : 0));
+    if (c == 0) scales[a] = r.scale;
+    from[i] = X.A + r.at * X.lda + 16 * c;
+    to[i] = SA::lds_offset(a, c);
+    deep[i] = 16 * c;
+  }
+#pragma unroll
+  for (int i = 0; i < SB::PER_THREAD; ++i) {
+    int a, c;
+    SB::chunk_of(i, tid, a, c);
+    int64_t column = n0 + a % TN;
+    if (column > X.n - 1) column = X.n - 1;
+    if (GATED && a >= TN) column += X.n;
+    from[SA::PER_THREAD + i] = X.B + tile.e * X.strideB + column * X.ldb + 16 * c;
+    to[SA::PER_THREAD + i] = TM * TK + SB::lds_offset(a, c);
+    deep[SA::PER_THREAD + i] = 16 * c;
+  }
+  constexpr int PIECES = SA::PER_THREAD + SB::PER_THREAD;
+  v4i held[PIECES];
+  auto load = [&](int64_t k0) {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      const int64_t left = X.k - k0 - deep[i];
+      held[i] = left >= 16 ? load16(from[i] + k0) : load16_partial(from[i] + k0, left > 0 ? (int)left : 0);
+    }
+  };
+  auto store = [&](int stage) {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) *reinterpret_cast<v4i *>(lds + stage * STAGE + to[i]) = held[i];
+  };
+  const int wm = wave >> 1, wn = wave & 1;
+  v16i acc[1 + GATED] = {};
+  const int64_t blocks = (X.k + TK - 1) / TK;
+  if (blocks > 0) {
+    load(0);
+    store(0);
+  }
+  __syncthreads();
+  for (int64_t t = 0; t < blocks; ++t) {
+    const bool more = t + 1 < blocks;
+    if (more) load((t + 1) * TK);
+    const uint8_t *sa = lds + (t & 1) * STAGE, *sb = sa + TM * TK;
+#pragma unroll
+    for (int ks = 0; ks < TK / 32; ++ks) {
+      const v4i a = SA::fragment(sa, wm * 32, ks, lane);
+#pragma unroll
+      for (int g = 0; g <= GATED; ++g) {
+        const v4i b = SB::fragment(sb, g * TN + wn * 32, ks, lane);
+        acc[g] = __builtin_amdgcn_mfma_i32_32x32x32_i8(b, a, acc[g], 0, 0, 0);
+      }
+    }
+    if (more) store((t + 1) & 1);
+    __syncthreads();
+  }
+  // lane l has row l % 32 of the wave's block and, of column group q, columns 8 q + 4 (l / 32) .. + 3
+  const int row = wm * 32 + (lane & 31);
+  if (row >= tile.count) return;
+  const float row_scale = scales[row];
+  const int64_t p = tile.first + row;
+  auto value = [&](int sum, int64_t column) {
+    const int64_t at = tile.e * outputs + column;
+    return linear_value(sum, row_scale, X.b_scales ? X.b_scales[at] : 1.0f, X.bias ? X.bias[at] : 0.0f);
+  };
+  auto activated = [&](float y) {
+    switch (activation_kind(X.act)) {
+      case 0: return Activate<0>::of(X.act)(y);
+      case 1: return Activate<1>::of(X.act)(y);
+      default: return Activate<2>::of(X.act)(y);
+    }
+  };
+#pragma unroll
+  for (int q = 0; q < 16; ++q) {
+    const int64_t j = n0 + wn * 32 + 8 * (q / 4) + 4 * (lane >> 5) + q % 4;
+    if (j >= X.n) continue;
+    float y = activated(value(acc[0][q], j));
+    if (GATED) y *= value(acc[GATED][q], X.n + j);
+    store_real(X.C, p * X.ldc + j, X.type, y);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_experts(const ExpertsArgs &X, hipStream_t s) {
+  // as many pieces as the experts' rows can be cut into; a grid has at most 65535 rows, and 2^32 - 1 threads a dimension
+  const int64_t slots = X.rows / TM + (X.experts < X.rows ? X.experts : X.rows);
+  const int64_t columns = (X.n + TN - 1) / TN;
+  constexpr int64_t MOST_X = 1 << 20, MOST_Y = 65535;
+  for (int64_t c = 0; c < columns; c += MOST_X)
+    for (int64_t slot = 0; slot < slots; slot += MOST_Y) {
+      Params P{X, slot, c * TN};
+      const dim3 grid((unsigned)(columns - c < MOST_X ? columns - c : MOST_X), (unsigned)(slots - slot < MOST_Y ? slots - slot : MOST_Y));
+      const hipError_t e = launch_with(X.gated ? reinterpret_cast<const void *>(experts_kernel<1>) : reinterpret_cast<const void *>(experts_kernel<0>),
+                                       grid, 256, 0, s, &P);
+      if (e != hipSuccess) return e;
+    }
+  return hipSuccess;
+}
+
+}  // namespace mip

@@ -14,7 +14,7 @@
 // four workgroups to a compute unit: 41 us from memory (3.3 TB/s), 39 resident, 30 without a norm.  A row of 4096: 2.5 us, of
 // which some 2 are the launch.
 #include "layer_internal.h"
-#include "real.h"
+#include "row_codes.h"
 
 namespace mip {
 
@@ -29,14 +29,6 @@ struct QuantizeParams {
   int64_t ldq;
   float *scales;
 };
-
-struct __attribute__((packed, aligned(1))) byte_oct { uint64_t v; };
-
-template <typename T>
-struct real_of;
-template <> struct real_of<float> { static constexpr int type = REAL_F32; };
-template <> struct real_of<__bf16> { static constexpr int type = REAL_BF16; };
-template <> struct real_of<_Float16> { static constexpr int type = REAL_F16; };
 
 // x_j and w_j of eight columns from j on; what lies behind the row is zero.
 template <typename T>
@@ -59,18 +51,6 @@ __device__ __forceinline__ void times_weight(const QuantizeParams &P, int64_t j,
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) x[e] = __fmul_rn(x[e], w[e]);
-}
-
-// The quotient 127 z / a, correctly rounded: the reciprocal r of a is, and one step of Newton's iteration on the quotient
-// then is as well (Markstein's theorem), where nothing underflows; then the nearest whole number, ties to even, in the
-// lowest byte (1.5 2^23 leaves no bits for fractions).
-__device__ __forceinline__ uint32_t code_of(float z, float by, float a, float r) {
-  const float num = __fmul_rn(z, by), q = num * r;
-  return __float_as_uint(__fadd_rn(__builtin_fmaf(__builtin_fmaf(-q, a, num), r, q), 12582912.0f));
-}
-// the lowest bytes of four words
-__device__ __forceinline__ uint32_t four_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
 }
 
 // WAVES to a row, ROWS rows to a workgroup; HELD: eights of columns a thread keeps, 0: none.
@@ -134,24 +114,9 @@ __global__ __launch_bounds__(64 * WAVES *ROWS) void quantize_kernel(QuantizePara
       scale *= __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(squares, (float)P.cols) + P.eps));
     P.scales[row] = scale;
   }
-  // far from 1, a power of two keeps the reciprocal and the products in range, and changes no quotient
-  const float by = top < 0x1p-60f ? 0x1p60f : (top > 0x1p60f ? 0x1p-60f : 1.0f);
+  const float by = code_range(top);
   const float a = top * by, by_127 = 127.0f * by, r = finite && top > 0.0f ? __fdiv_rn(1.0f, a) : 0.0f;
-  auto put = [&](int64_t j, float (&v)[8]) {
-    uint32_t n[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) n[e] = code_of(v[e], by_127, a, r);
-    const uint64_t both = (uint64_t)four_bytes(n[4], n[5], n[6], n[7]) << 32 | four_bytes(n[0], n[1], n[2], n[3]);
-    const uint64_t word = r != 0.0f ? both : 0;
-    int8_t *q = P.Q + row * P.ldq + j;
-    if (j + 8 <= P.cols) {
-      reinterpret_cast<byte_oct *>(q)->v = word;
-    } else {
-#pragma unroll
-      for (int e = 0; e < 7; ++e)
-        if (j + e < P.cols) q[e] = (int8_t)(word >> (8 * e));
-    }
-  };
+  auto put = [&](int64_t j, float (&v)[8]) { put_codes(P.Q + row * P.ldq + j, P.cols - j, v, by_127, a, r); };
   if (HELD) {
 #pragma unroll
     for (int u = 0; u < HELD; ++u) {

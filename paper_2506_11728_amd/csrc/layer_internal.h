@@ -51,4 +51,49 @@ AttentionKernel attention_wide(int head_dim, int type, int log_page);
 hipError_t launch_attention(AttentionArgs P, int requests, int head_dim, int type, void *ws, size_t ws_bytes, hipStream_t s);
 size_t attention_scratch(int64_t requests, int64_t kv_heads, int64_t shared, int head_dim, int64_t max_q, int64_t max_kv);
 
+// ---- a mixture of experts ----
+
+constexpr int64_t MOST_EXPERTS = 1024, MOST_CHOSEN = 32, MOST_GROUPS = 64;
+
+struct RouteArgs {
+  const void *logits;
+  const float *bias;  // null: none
+  int32_t *ids;
+  float *weights;
+  int32_t *starts, *order, *places;  // starts null: the rows are not sorted; order, places null: not written
+  uint8_t *counts, *ranks;           // the launcher's own: of each block of tokens, rows of an expert, and a row's place among them
+  int64_t ldl, tokens;
+  int experts, top, groups, top_groups, best, normalise, sigmoid;
+  Divisor each;  // experts of a group
+  float scale;
+};
+size_t route_scratch(int64_t tokens, int64_t experts, int64_t top);
+hipError_t launch_route(RouteArgs P, int type, void *ws, hipStream_t s);
+
+struct ExpertsArgs {
+  const uint8_t *A, *B;
+  const float *a_scales, *b_scales, *bias;  // null: 1, 1, 0
+  const int32_t *starts, *order;            // order null: row p of A is row p
+  void *C;
+  int64_t lda, ldb, strideB, ldc, a_rows, rows, n, k;
+  int experts, act, gated, type;
+  Divisor top;
+};
+hipError_t launch_experts(const ExpertsArgs &P, hipStream_t s);
+
+enum RowNorm { ROW_NORM_NONE = 0, ROW_NORM_RMS = 1, ROW_NORM_LAYER = 2 };
+
+struct JoinArgs {
+  const void *X, *gate, *R;
+  void *H, *N;
+  int8_t *Q;
+  float *scales;
+  const int32_t *places;
+  const float *weights, *post_weight, *post_bias, *norm_weight, *norm_bias;
+  int64_t rows, row0, ldx, x_rows, ldg, gate_rows, ldr, ldh, ldn, ldq;
+  int cols, parts, post_norm, norm;
+  float scale, eps;
+};
+hipError_t launch_join(JoinArgs P, int type, hipStream_t s);
+
 }  // namespace mip

@@ -31,15 +31,20 @@ typedef int (*rope_fn)(q, q, q, q, int, p, q, p, q, p, q, p, p, float, p, p, q, 
 typedef int (*kv4_read_fn)(q, q, q, int, p, size_t, q, q, p, p, q, p, q, p);
 typedef int (*attention_fn)(q, q, q, q, int, p, q, q, p, q, p, q, p, size_t, q, q, p, q, float, p, q, p, size_t, p);
 
+typedef int (*route_fn)(q, q, q, p, q, int, p, int, q, q, q, int, float, p, p, p, p, p, p, size_t, p);
+typedef int (*experts_fn)(q, q, q, q, p, q, q, p, p, p, q, p, q, q, p, p, int, int, p, q, int, p);
+typedef int (*join_fn)(q, q, q, int, p, q, q, p, p, int, p, p, p, q, q, float, p, q, p, q, int, p, p, float, p, q, p, q, p, p);
+
 enum { GEMM, GEMM_SCALED, BATCHED, PACKED, CONV, CONV_SCALED, CONV_SUMS, CONV_SCALED_SUMS,
-       QUANTIZE, LINEAR, ROPE, KV4_READ, ATTENTION, KINDS };
+       QUANTIZE, LINEAR, ROPE, KV4_READ, ATTENTION, ROUTE, EXPERTS, JOIN, KINDS };
 
 /* q int64, i int, p pointer, z size, s stream, f float: the arguments of each kind in order */
 static const char *const kFormat[KINDS] = {
     "qqqpqipqipqiipzs",  "qqqpqipqipqiipzsf", "qqqpqiqpqiqpqiqqipzs", "qqqpqippqiipzs",
     "qqqqqqqqqpppipzs",  "qqqqqqqqqpppipzsf", "qqqqqqqqqpppipzsp",    "qqqqqqqqqpppipzsfp",
     "qqpqipfpqps", "qqqpqppqippipqpqipzs", "qqqqipqpqpqppfppqqippqpqpzqqps", "qqqipzqqppqpqs",
-    "qqqqipqqpqpqpzqqpqfpqpzs"};
+    "qqqqipqqpqpqpzqqpqfpqpzs", "qqqpqipiqqqifppppppzs", "qqqqpqqpppqpqqppiipqis",
+    "qqqipqqppipppqqfpqpqippfpqpqps"};
 #define MOST_ARGS 30
 
 typedef union { q i; p ptr; float f; } value;
@@ -164,6 +169,19 @@ static PyObject *call(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
       break;
     case KV4_READ:
       rc = ((kv4_read_fn)e->fn)(Q(0), Q(1), Q(2), I(3), P(4), Z(5), Q(6), Q(7), P(8), P(9), Q(10), P(11), Q(12), P(13));
+      break;
+    case ROUTE:
+      rc = ((route_fn)e->fn)(Q(0), Q(1), Q(2), P(3), Q(4), I(5), P(6), I(7), Q(8), Q(9), Q(10), I(11), F(12), P(13),
+                             P(14), P(15), P(16), P(17), P(18), Z(19), P(20));
+      break;
+    case EXPERTS:
+      rc = ((experts_fn)e->fn)(Q(0), Q(1), Q(2), Q(3), P(4), Q(5), Q(6), P(7), P(8), P(9), Q(10), P(11), Q(12), Q(13),
+                               P(14), P(15), I(16), I(17), P(18), Q(19), I(20), P(21));
+      break;
+    case JOIN:
+      rc = ((join_fn)e->fn)(Q(0), Q(1), Q(2), I(3), P(4), Q(5), Q(6), P(7), P(8), I(9), P(10), P(11), P(12), Q(13),
+                            Q(14), F(15), P(16), Q(17), P(18), Q(19), I(20), P(21), P(22), F(23), P(24), Q(25), P(26),
+                            Q(27), P(28), P(29));
       break;
     default:
       rc = ((attention_fn)e->fn)(Q(0), Q(1), Q(2), Q(3), I(4), P(5), Q(6), Q(7), P(8), Q(9), P(10), Q(11), P(12), Z(13),
