@@ -116,9 +116,7 @@ __global__ __launch_bounds__(256) void experts_kernel(Params P) {
   }
 }
 
-}  // namespace
-
-hipError_t launch_experts(const ExpertsArgs &X, hipStream_t s) {
+hipError_t launch_unaligned(const ExpertsArgs &X, hipStream_t s) {
   // as many pieces as the experts' rows can be cut into; a grid has at most 65535 rows, and 2^32 - 1 threads a dimension
   const int64_t slots = X.rows / TM + (X.experts < X.rows ? X.experts : X.rows);
   const int64_t columns = (X.n + TN - 1) / TN;
@@ -132,6 +130,20 @@ hipError_t launch_experts(const ExpertsArgs &X, hipStream_t s) {
       if (e != hipSuccess) return e;
     }
   return hipSuccess;
+}
+
+}  // namespace
+
+// The host knows the rows of all experts together and no expert's.  16 rows to a workgroup where an expert has few on average, or where so few
+// workgroups result that the device would not be full with larger ones: each reads its weights once, by itself (64 experts' 1024
+// pairs of columns of 2048, 8 rows each on average 57.3 us, with tiles 63.2; 12 rows 61.9 and 60.0; 16 rows 69.7 and 63.5; 8 experts' 4096 columns of 4096,
+// 16 rows each 36.7 and 39.2, 32 rows 49.7 and 40.0).  Else tiles of rows that can be streamed: 128 x 128, two workgroups to a compute
+// unit, so that one's first loads and write-back go on beside the other's products; under a long k of many rows 192 x 256, which load less for a product (8 experts,
+// 512 rows each on average, 4096 columns of 11008: 221 us against 239; 1024 pairs of columns of 2048, 64 experts: 222 against 201).
+hipError_t launch_experts(const ExpertsArgs &X, hipStream_t s) {
+  if ((X.rows <= 12 * X.experts || experts_slim_tiles(X) <= 1024) && experts_slim_eligible(X)) return launch_experts_slim(X, s);
+  if (experts_tile_eligible(X)) return launch_experts_tile(X, X.k >= 4096 && X.rows >= 384 * X.experts, s);
+  return launch_unaligned(X, s);
 }
 
 }  // namespace mip

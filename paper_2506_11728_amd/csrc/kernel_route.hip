@@ -48,18 +48,34 @@ __device__ __forceinline__ float wave_sum(float v) {
   v += moved<BROADCAST_31, 0xc>(v, 0.0f);
   return last_lane(v);
 }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved(double x, double other) {
+  const long long v = __double_as_longlong(x), o = __double_as_longlong(other);
+  const int lo = __builtin_amdgcn_update_dpp((int)o, (int)v, CTRL, ROWS, 0xf, false);
+  const int hi = __builtin_amdgcn_update_dpp((int)(o >> 32), (int)(v >> 32), CTRL, ROWS, 0xf, false);
+  return __longlong_as_double((long long)hi << 32 | (unsigned)lo);
+}
+__device__ __forceinline__ double last_lane(double x) {
+  const long long v = __double_as_longlong(x);
+  const int lo = __builtin_amdgcn_readlane((int)v, 63), hi = __builtin_amdgcn_readlane((int)(v >> 32), 63);
+  return __longlong_as_double((long long)hi << 32 | (unsigned)lo);
+}
 __device__ __forceinline__ double wave_most(double v) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const double o = __shfl_xor(v, d);
-    v = o > v ? o : v;
-  }
-  return v;
+  auto larger = [](double a, double b) { return a > b ? a : b; };
+  v = larger(v, moved<SHR_1, 0xf>(v, v));
+  v = larger(v, moved<SHR_2, 0xf>(v, v));
+  v = larger(v, moved<SHR_4, 0xf>(v, v));
+  v = larger(v, moved<SHR_8, 0xf>(v, v));
+  v = larger(v, moved<BROADCAST_15, 0xa>(v, v));
+  return last_lane(larger(v, moved<BROADCAST_31, 0xc>(v, v)));
 }
 __device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-  return v;
+  v += moved<SHR_1, 0xf>(v, 0.0);
+  v += moved<SHR_2, 0xf>(v, 0.0);
+  v += moved<SHR_4, 0xf>(v, 0.0);
+  v += moved<SHR_8, 0xf>(v, 0.0);
+  v += moved<BROADCAST_15, 0xa>(v, 0.0);
+  return last_lane(v + moved<BROADCAST_31, 0xc>(v, 0.0));
 }
 
 constexpr float NONE = -__builtin_inff();
@@ -144,9 +160,9 @@ __device__ __forceinline__ bool choose(const RouteArgs &P, K (&c)[PER], const fl
   return doubt;
 }
 
-// One token: lane j < top gets its j-th expert (-1: none) and its weight.
+// One token: lane j < top gets its j-th expert (-1: none) and its weight.  doubted: float32 has been tried.
 template <int PER>
-__device__ __forceinline__ void route_token(const RouteArgs &P, int type, int64_t token, int lane, int *id, float *weight) {
+__device__ __forceinline__ void route_token(const RouteArgs &P, int type, int64_t token, int lane, bool doubted, int *id, float *weight) {
   float x[PER];
   float largest = NONE;
   bool lost = false;
@@ -194,7 +210,7 @@ __device__ __forceinline__ void route_token(const RouteArgs &P, int type, int64_
       // additions, and its terms' arguments, 7 2^-23 of it) and the reciprocal are off, below 2^-18 of it together.  The addition of the bias.
       const float most = wave_most(size);
       const float wrong = (P.sigmoid ? 0x1p-22f : 0x1p-18f * __builtin_amdgcn_rcpf(all)) + most * 0x1p-24f;
-      if (choose<float, PER>(P, c, x, 2.0f * wrong, lane, &chosen)) {
+      if (doubted || choose<float, PER>(P, c, x, 2.0f * wrong, lane, &chosen)) {
         double d[PER], sum = 0.0;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
@@ -234,6 +250,217 @@ __device__ __forceinline__ void route_token(const RouteArgs &P, int type, int64_
   *weight = w;
 }
 
+// ---- four tokens to a wave ----
+// A row of 16 lanes takes a token, lane q the experts PER q .. PER q + PER - 1: what is done once for a token, the steps of a
+// maximum above all, is done for four at a time.
+
+template <int BY>
+__device__ __forceinline__ float turned(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + BY, 0xf, 0xf, true)); }
+template <int BY>
+__device__ __forceinline__ int turned(int x) { return __builtin_amdgcn_update_dpp(0, x, 0x120 + BY, 0xf, 0xf, true); }
+__device__ __forceinline__ float row_most(float v) {
+  v = __builtin_fmaxf(v, turned<8>(v));
+  v = __builtin_fmaxf(v, turned<4>(v));
+  v = __builtin_fmaxf(v, turned<2>(v));
+  return __builtin_fmaxf(v, turned<1>(v));
+}
+__device__ __forceinline__ int row_least(int v) {
+  v = min(v, turned<8>(v));
+  v = min(v, turned<4>(v));
+  v = min(v, turned<2>(v));
+  return min(v, turned<1>(v));
+}
+__device__ __forceinline__ float row_sum(float v) {
+  v += turned<8>(v);
+  v += turned<4>(v);
+  v += turned<2>(v);
+  return v + turned<1>(v);
+}
+__device__ __forceinline__ bool any_of_row(bool b, int lane) { return ((__ballot(b) >> (lane & 48)) & 0xffff) != 0; }
+
+// How many of the row's other lanes have a larger v, or the same and a smaller number.
+template <int D = 1>
+__device__ __forceinline__ int larger_in_row(float v, int number) {
+  if constexpr (D > 15) {
+    return 0;
+  } else {
+    const float o = turned<D>(v);
+    const int n = turned<D>(number);
+    return (o > v || (o == v && n < number) ? 1 : 0) + larger_in_row<D + 1>(v, number);
+  }
+}
+
+template <int BY>
+__device__ __forceinline__ double turned(double x) {
+  return moved<0x120 + BY, 0xf>(x, x);
+}
+template <int D = 1>
+__device__ __forceinline__ int larger_in_row(double v, int number) {
+  if constexpr (D > 15) {
+    return 0;
+  } else {
+    const double o = turned<D>(v);
+    const int n = turned<D>(number);
+    return (o > v || (o == v && n < number) ? 1 : 0) + larger_in_row<D + 1>(v, number);
+  }
+}
+
+// Lane q < top (at most 15) gets its token's q-th expert (-1: none) and its weight; returns whether the token has to be done again, in float64.
+// With groups: one or more whole lanes to a group, 1, 2, 4 or 8.
+template <int PER>
+__device__ __forceinline__ bool route_row(const RouteArgs &P, int type, int64_t token, int lane, int *id, float *weight) {
+  const int q = lane & 15, first = q * PER;
+  const int64_t at = token * P.ldl + first;
+  float x[PER], bias[PER];
+  bool lost = false;
+  float largest = NONE;
+#pragma unroll
+  for (int i = 0; i < PER; i += 4) {
+    if (first + i + 4 <= P.experts) {
+      const v4f four = load_real4(P.logits, at + i, type);
+      const v4f more = P.bias ? load_real4(P.bias, first + i, REAL_F32) : v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        x[i + k] = four[k];
+        bias[i + k] = more[k];
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const bool here = first + i + k < P.experts;
+        x[i + k] = here ? load_real(P.logits, at + i + k, type) : NONE;
+        bias[i + k] = here && P.bias ? P.bias[first + i + k] : 0.0f;
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    lost |= x[i] != x[i];
+    largest = __builtin_fmaxf(largest, x[i]);
+  }
+  largest = row_most(largest);
+  if (!P.sigmoid) lost |= largest == __builtin_inff();
+  const bool summed = P.groups > 1 && P.best == 2, scored = P.bias || summed;
+  float all = 1.0f;  // softmax: the sum of all exponentials
+  if (!P.sigmoid && (!P.normalise || scored)) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) sum += x[i] > NONE ? expf(x[i] - largest) : 0.0f;
+    all = row_sum(sum);
+  }
+  float c[PER], near = -1.0f;
+  if (!scored) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) c[i] = x[i];
+  } else {
+    const float over = P.sigmoid ? 1.0f : __builtin_amdgcn_rcpf(all);
+    float size = 0.0f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      lost |= bias[i] != bias[i];
+      if (P.sigmoid) c[i] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * x[i]));
+      else c[i] = __builtin_amdgcn_exp2f(1.4426950408889634f * (x[i] - largest)) * over;
+      c[i] += bias[i];
+      c[i] = x[i] > NONE ? c[i] : NONE;
+      size = c[i] > NONE ? __builtin_fmaxf(size, __builtin_fabsf(c[i])) : size;
+    }
+    near = 2.0f * ((P.sigmoid ? 0x1p-22f : 0x1p-18f * over) + row_most(size) * 0x1p-24f);  // (as in route_token)
+  }
+  lost = any_of_row(lost, lane);
+  bool doubt = false;
+  if (P.groups > 1) {
+    const int span = (int)P.each.d / PER, group = q / span;
+    float one = c[0], two = NONE;
+#pragma unroll
+    for (int i = 1; i < PER; ++i) {
+      two = __builtin_fmaxf(two, __builtin_fminf(one, c[i]));
+      one = __builtin_fmaxf(one, c[i]);
+    }
+    auto join = [&](float o1, float o2) {
+      two = __builtin_fmaxf(__builtin_fmaxf(two, o2), __builtin_fminf(one, o1));
+      one = __builtin_fmaxf(one, o1);
+    };
+    // (lane ^ 1, ^ 2; then the other half of eight and of sixteen lanes, whose quarters have the same by now)
+    if (span > 1) join(moved<0xb1, 0xf>(one, one), moved<0xb1, 0xf>(two, two));
+    if (span > 2) join(moved<0x4e, 0xf>(one, one), moved<0x4e, 0xf>(two, two));
+    if (span > 4) join(moved<0x141, 0xf>(one, one), moved<0x141, 0xf>(two, two));
+    const float score = one > NONE ? (P.best == 2 && two > NONE ? one + two : one) : NONE;
+    const int ahead = larger_in_row(score, group);  // (by all lanes: one that is switched off has nothing to give)
+    const bool kept = score > NONE && ahead < P.top_groups * span;
+    const float least = -row_most(kept ? -score : NONE), next = row_most(kept ? NONE : score);
+    doubt = next > NONE && least - next <= 4.0f * near;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) c[i] = kept ? c[i] : NONE;
+  }
+  int mine = -1;
+  float before = NONE;
+  bool unsure = false;  // of the order of those that are chosen, and of the next one
+  auto most_left = [&]() {
+    float own = c[0];
+#pragma unroll
+    for (int i = 1; i < PER; ++i) own = __builtin_fmaxf(own, c[i]);
+    return row_most(own);
+  };
+  const int turns = P.top + (scored ? 1 : 0);
+  for (int j = 0; j < turns; ++j) {
+    const float most = most_left();
+    const bool found = most > NONE;
+    unsure |= j > 0 && found && before - most <= near;
+    before = most;
+    int key = PER;
+#pragma unroll
+    for (int i = PER - 1; i >= 0; --i) key = c[i] == most ? i : key;
+    const int winner = row_least(key < PER ? first + key : 1 << 20);
+    if (q == j && found) mine = winner;
+    const int local = winner - first;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) c[i] = local == i ? NONE : c[i];
+  }
+  unsure = unsure && !lost;
+  if (__ballot(unsure)) {
+    // Those that were chosen and the next one, in the order of their exact c: one to a lane.  (Where one more is as near, it is all done again.)
+    const float most = most_left();
+    doubt |= unsure && most > NONE && before - most <= near;
+    double sum = 1.0;
+    if (!P.sigmoid) {
+      sum = 0.0;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) sum += x[i] > NONE ? exp((double)x[i] - (double)largest) : 0.0;
+      sum += turned<8>(sum);
+      sum += turned<4>(sum);
+      sum += turned<2>(sum);
+      sum += turned<1>(sum);
+    }
+    double exact = (double)NONE;
+    const int number = mine >= 0 ? mine : (1 << 20) + q;
+    if (mine >= 0 && !lost) {
+      const double l = load_real(P.logits, token * P.ldl + mine, type);
+      exact = P.sigmoid ? 1.0 / (1.0 + exp(-l)) : exp(l - (double)largest) / sum;
+      if (P.bias) exact += (double)P.bias[mine];
+    }
+    const int rank = larger_in_row(exact, number);
+    const int sorted = __builtin_amdgcn_ds_permute(((lane & 48) + rank) * 4, number);
+    if (unsure) mine = sorted < (1 << 20) ? sorted : -1;
+  }
+  if (q >= P.top) mine = -1;
+  if (lost) {
+    mine = -1;
+    doubt = false;
+  }
+  const bool any = mine >= 0;
+  const float logit = any ? load_real(P.logits, token * P.ldl + mine, type) : NONE;
+  const float top = row_most(logit);
+  const bool ratio = P.normalise && (!P.sigmoid || top < -40.0f);
+  float s;
+  if (P.sigmoid && !ratio) s = logit < -40.0f ? expf(logit) : __fdiv_rn(1.0f, 1.0f + expf(-logit));
+  else s = expf(logit - (ratio ? top : largest));
+  if (!any) s = 0.0f;
+  const float over = P.normalise ? row_sum(s) : (P.sigmoid ? 1.0f : all);
+  *id = mine;
+  *weight = lost ? __builtin_nanf("") : (any ? P.scale * __fdiv_rn(s, over) : 0.0f);
+  return doubt;
+}
+
 // Sums of what lies before this thread's number among those of the workgroup.  All threads call it.
 __device__ __forceinline__ int before_in_group(int n, int *waves, int tid) {
   const int lane = tid & 63, wave = tid >> 6;
@@ -252,27 +479,44 @@ __device__ __forceinline__ int before_in_group(int n, int *waves, int tid) {
   return first + sum - n;
 }
 
-template <int PER>
-__global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs P, int type) {
+// FOUR: four tokens to a wave, for more than 32 tokens.
+template <int PER, bool FOUR>
+__global__ __launch_bounds__(FOUR ? 512 : THREADS) void route_kernel(RouteArgs P, int type) {
+  constexpr int OWN = FOUR ? 512 : THREADS;  // threads
   __shared__ uint32_t has[64 * PER];
   __shared__ int ids[TOKENS * MOST_CHOSEN];
-  __shared__ int waves[WAVES], first[64 * PER];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t token0 = (int64_t)blockIdx.x * TOKENS;
   const int tokens = (int)(P.tokens - token0 < TOKENS ? P.tokens - token0 : TOKENS);
   if (P.starts) {
-    for (int e = tid; e < 64 * PER; e += THREADS) has[e] = 0;
+    for (int e = tid; e < 64 * PER; e += OWN) has[e] = 0;
     __syncthreads();
   }
-  for (int t = wave; t < tokens; t += WAVES) {
-    int id;
-    float w;
-    route_token<PER>(P, type, token0 + t, lane, &id, &w);
-    if (lane < P.top) {
-      P.ids[(token0 + t) * P.top + lane] = id;
-      P.weights[(token0 + t) * P.top + lane] = w;
-      ids[t * P.top + lane] = id;
-      if (P.starts && id >= 0) atomicOr(&has[id], 1u << t);
+  // lane j has the j-th choice of token t of the workgroup
+  auto put = [&](int t, int j, int id, float w) {
+    P.ids[(token0 + t) * P.top + j] = id;
+    P.weights[(token0 + t) * P.top + j] = w;
+    ids[t * P.top + j] = id;
+    if (P.starts && id >= 0) atomicOr(&has[id], 1u << t);
+  };
+  int id;
+  float w;
+  if constexpr (FOUR) {
+    const int t0 = 4 * wave, t = t0 + (lane >> 4);
+    if (t0 < tokens) {
+      const bool again = route_row<4 * PER>(P, type, token0 + (t < tokens ? t : tokens - 1), lane, &id, &w);
+      const uint64_t rows = __ballot(again && t < tokens);
+      if (t < tokens && !again && (lane & 15) < P.top) put(t, lane & 15, id, w);
+      for (int r = 0; r < 4; ++r) {
+        if (!((rows >> (16 * r)) & 1)) continue;
+        route_token<PER>(P, type, token0 + t0 + r, lane, true, &id, &w);
+        if (lane < P.top) put(t0 + r, lane, id, w);
+      }
+    }
+  } else {
+    for (int t = wave; t < tokens; t += WAVES) {
+      route_token<PER>(P, type, token0 + t, lane, false, &id, &w);
+      if (lane < P.top) put(t, lane, id, w);
     }
   }
   if (!P.starts) return;
@@ -280,38 +524,54 @@ __global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs P, int type) {
   const int rows = tokens * P.top;
   if (P.counts) {  // for the second kernel
     const int padded = (P.experts + 3) & ~3;
-    for (int e = tid; e < padded; e += THREADS)
+    for (int e = tid; e < padded; e += OWN)
       P.counts[(int64_t)blockIdx.x * padded + e] = e < P.experts ? (uint8_t)__popc(has[e]) : 0;
-    for (int i = tid; i < rows; i += THREADS) {
+    for (int i = tid; i < rows; i += OWN) {
       const int id = ids[i];
       if (id >= 0) P.ranks[token0 * P.top + i] = (uint8_t)__popc(has[id] & ((1u << (i / P.top)) - 1));
     }
     return;
   }
-  const int mine = tid < P.experts ? __popc(has[tid]) : 0;
-  const int from = before_in_group(mine, waves, tid);
-  if (tid < P.experts) {
-    first[tid] = from;
-    P.starts[tid] = from;
-    if (tid == P.experts - 1) P.starts[P.experts] = from + mine;
-  }
-  __syncthreads();
-  for (int i = tid; i < rows; i += THREADS) {
-    const int id = ids[i];
-    const int at = id < 0 ? -1 : first[id] + __popc(has[id] & ((1u << (i / P.top)) - 1));
-    if (P.places) P.places[i] = at;
-    if (P.order && at >= 0) P.order[at] = i;
+  if constexpr (!FOUR) {
+    __shared__ int waves[WAVES], first[64 * PER];
+    const int mine = tid < P.experts ? __popc(has[tid]) : 0;
+    const int from = before_in_group(mine, waves, tid);
+    if (tid < P.experts) {
+      first[tid] = from;
+      P.starts[tid] = from;
+      if (tid == P.experts - 1) P.starts[P.experts] = from + mine;
+    }
+    __syncthreads();
+    for (int i = tid; i < rows; i += THREADS) {
+      const int id = ids[i];
+      const int at = id < 0 ? -1 : first[id] + __popc(has[id] & ((1u << (i / P.top)) - 1));
+      if (P.places) P.places[i] = at;
+      if (P.order && at >= 0) P.order[at] = i;
+    }
   }
 }
 
 // The second kernel: workgroup b puts the rows of the `blocks` blocks of tokens from b * blocks on in their places.
-constexpr int AT_ONCE = 8;  // blocks whose first places are in LDS together
 __global__ __launch_bounds__(THREADS) void place_kernel(RouteArgs P, int64_t all_blocks, int blocks) {
   __shared__ int total[MOST_EXPERTS], before[MOST_EXPERTS], waves[WAVES];
-  __shared__ int first[AT_ONCE][MOST_EXPERTS];
+  __shared__ int first[MOST_EXPERTS];
   const int tid = threadIdx.x, padded = (P.experts + 3) & ~3, words = padded / 4;
   const int64_t block0 = (int64_t)blockIdx.x * blocks;
   const int64_t block1 = block0 + blocks < all_blocks ? block0 + blocks : all_blocks;
+  // what is needed of a block of tokens behind the sums, sent for before them: a row to a thread, and an expert's count
+  static_assert(TOKENS * MOST_CHOSEN <= THREADS && MOST_EXPERTS <= THREADS, "one of each to a thread");
+  const int rows = TOKENS * P.top;
+  int id = -1, rank = 0, count = 0;
+  auto fetch = [&](int64_t b) {
+    const int64_t i = b * rows + tid;
+    id = -1;
+    if (tid < rows && i < P.tokens * P.top) {
+      id = P.ids[i];
+      rank = P.ranks[i];
+    }
+    count = tid < P.experts ? P.counts[b * padded + tid] : 0;
+  };
+  fetch(block0);
   total[tid] = before[tid] = 0;
   __syncthreads();
   // four experts to a thread, the blocks among as many threads as there are for it
@@ -321,14 +581,18 @@ __global__ __launch_bounds__(THREADS) void place_kernel(RouteArgs P, int64_t all
   if (word < words) {
     const uint32_t *counts = reinterpret_cast<const uint32_t *>(P.counts);
     int sum[4] = {0, 0, 0, 0}, sum_before[4] = {0, 0, 0, 0};
-#pragma unroll 8
-    for (int64_t b = part; b < all_blocks; b += parts) {
-      const uint32_t four = counts[b * words + word];
-      const uint32_t mask = b < block0 ? ~0u : 0u;
+    for (int64_t b0 = part; b0 < all_blocks; b0 += 16 * parts) {
+      uint32_t four[16];  // (all on their way before the first is used)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        sum[i] += (four >> (8 * i)) & 0xff;
-        sum_before[i] += ((four & mask) >> (8 * i)) & 0xff;
+      for (int u = 0; u < 16; ++u) four[u] = b0 + u * parts < all_blocks ? counts[(b0 + u * parts) * words + word] : 0u;
+#pragma unroll
+      for (int u = 0; u < 16; ++u) {
+        const uint32_t earlier = b0 + u * parts < block0 ? four[u] : 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          sum[i] += (four[u] >> (8 * i)) & 0xff;
+          sum_before[i] += (earlier >> (8 * i)) & 0xff;
+        }
       }
     }
 #pragma unroll
@@ -345,24 +609,16 @@ __global__ __launch_bounds__(THREADS) void place_kernel(RouteArgs P, int64_t all
     if (tid == P.experts - 1) P.starts[P.experts] = from + mine;
   }
   int next = from + before[tid];  // the first place of expert tid's rows in the next block
-  for (int64_t b0 = block0; b0 < block1; b0 += AT_ONCE) {
-    const int count = (int)(block1 - b0 < AT_ONCE ? block1 - b0 : AT_ONCE);
-    if (tid < P.experts) {
-#pragma unroll
-      for (int b = 0; b < AT_ONCE; ++b) {
-        if (b >= count) break;
-        first[b][tid] = next;
-        next += P.counts[(b0 + b) * padded + tid];
-      }
-    }
+  for (int64_t b = block0; b < block1; ++b) {
+    first[tid] = next;
+    next += count;
     __syncthreads();
-    const int64_t row0 = b0 * TOKENS * P.top, end = (b0 + count) * TOKENS < P.tokens ? (b0 + count) * TOKENS * P.top : P.tokens * P.top;
-    for (int64_t i = row0 + tid; i < end; i += THREADS) {
-      const int id = P.ids[i];
-      const int at = id < 0 ? -1 : first[(int)(i - row0) / (TOKENS * P.top)][id] + P.ranks[i];
-      if (P.places) P.places[i] = at;
-      if (P.order && at >= 0) P.order[at] = (int)i;
-    }
+    const int64_t i = b * rows + tid;
+    const int at = id < 0 ? -1 : first[id] + rank;
+    const bool here = tid < rows && i < P.tokens * P.top;
+    if (b + 1 < block1) fetch(b + 1);
+    if (here && P.places) P.places[i] = at;
+    if (here && P.order && at >= 0) P.order[at] = (int)i;
     __syncthreads();
   }
 }
@@ -384,16 +640,23 @@ hipError_t launch_route(RouteArgs P, int type, void *ws, hipStream_t s) {
     P.counts = static_cast<uint8_t *>(ws);
     P.ranks = P.counts + counts_bytes(P.tokens, P.experts);
   }
-  void (*kernel)(RouteArgs, int) = P.experts <= 64 ? route_kernel<1> : P.experts <= 128 ? route_kernel<2> : P.experts <= 256 ? route_kernel<4>
-                                   : P.experts <= 512 ? route_kernel<8> : route_kernel<16>;
+  // Four tokens to a wave (517 tokens, 60 experts 7.6 -> 5.1 us, 8192 and 256 12.3 -> 7.8); up to 32 a token has a wave of its own, which is sooner done.
+  const int per = P.experts <= 64 ? 1 : P.experts <= 128 ? 2 : P.experts <= 256 ? 4 : P.experts <= 512 ? 8 : 16;
+  const int each = (int)P.each.d, span = each / (4 * per);
+  const bool four = P.tokens > TOKENS && per <= 4 && P.top <= 15 &&
+                    (P.groups == 1 || (each % (4 * per) == 0 && (span == 1 || span == 2 || span == 4 || span == 8)));
+  void (*kernel)(RouteArgs, int) = per == 1   ? (four ? route_kernel<1, true> : route_kernel<1, false>)
+                                   : per == 2 ? (four ? route_kernel<2, true> : route_kernel<2, false>)
+                                   : per == 4 ? (four ? route_kernel<4, true> : route_kernel<4, false>)
+                                   : per == 8 ? route_kernel<8, false> : route_kernel<16, false>;
   void *list[] = {&P, &type};
-  hipError_t e = hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3((unsigned)blocks), dim3(THREADS), list, 0, s);
+  hipError_t e = hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3((unsigned)blocks), dim3(four ? 512 : THREADS), list, 0, s);
   if (e == hipSuccess && P.counts) {
-    const int64_t groups = blocks / AT_ONCE < 256 ? (blocks + AT_ONCE - 1) / AT_ONCE : 256;
+    const int64_t groups = blocks < 256 ? blocks : 256;  // (each adds up all counts)
     int64_t all = blocks;
-    int each = (int)((blocks + groups - 1) / groups);
-    void *more[] = {&P, &all, &each};
-    e = hipLaunchKernel(reinterpret_cast<const void *>(place_kernel), dim3((unsigned)((blocks + each - 1) / each)), dim3(THREADS), more, 0, s);
+    int share = (int)((blocks + groups - 1) / groups);
+    void *more[] = {&P, &all, &share};
+    e = hipLaunchKernel(reinterpret_cast<const void *>(place_kernel), dim3((unsigned)((blocks + share - 1) / share)), dim3(THREADS), more, 0, s);
   }
   if (e != hipSuccess) (void)hipGetLastError();  // (the caller gets it; the next check of theirs must not find it again)
   return e;
