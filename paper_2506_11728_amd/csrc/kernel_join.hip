@@ -8,6 +8,7 @@
 // float64, from the registers.
 #include "layer_internal.h"
 #include "row_codes.h"
+#include "wave.h"
 
 namespace mip {
 
@@ -17,15 +18,12 @@ struct TwoSums {
   float a, b;
 };
 
-// Sums over the threads of a row, in the same order every time.  `room`: WAVES words twice, of which the calls use the halves in turn, so that one
-// barrier to a call is enough.
+// Sums over the threads of a row, in the same order every time.  `room`: two words to a wave, of this call's own, so that one barrier is
+// enough.
 template <int WAVES>
-__device__ __forceinline__ TwoSums row_sums(TwoSums s, float (*room)[2], int wave, int lane) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    s.a += __shfl_xor(s.a, d);
-    s.b += __shfl_xor(s.b, d);
-  }
+__device__ __forceinline__ TwoSums row_sums(TwoSums s, bool both, float (*room)[2], int wave, int lane) {
+  if (both) s.a = wave_sum(s.a);
+  s.b = wave_sum(s.b);
   if constexpr (WAVES > 1) {
     if (lane == 0) {
       room[wave][0] = s.a;
@@ -78,36 +76,87 @@ __device__ __forceinline__ void store_part(void *p, int64_t at, int64_t count, c
   }
 }
 
-// WAVES to a row, ROWS rows to a workgroup; HELD: eights of columns a thread keeps.
-template <typename T, int WAVES, int ROWS, int HELD>
+template <typename T>
+struct eight_of {
+  typedef T type __attribute__((ext_vector_type(8)));
+};
+
+// WAVES to a row, ROWS rows to a workgroup; HELD: eights of columns a thread keeps.  WHOLE: the columns are a multiple of eight, so that
+// a thread's eights are there or are not; what lies behind the row is zero throughout.
+template <typename T, int WAVES, int ROWS, int HELD, bool WHOLE>
 __global__ __launch_bounds__(64 * WAVES *ROWS) void join_kernel(JoinArgs P) {
   constexpr int THREADS = 64 * WAVES;
+  typedef typename eight_of<T>::type Eight;
+  typedef float v8f __attribute__((ext_vector_type(8)));
   __shared__ float sums[4][WAVES * ROWS][2];
   __shared__ double wide_sums[WAVES * ROWS];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64 % WAVES, at = threadIdx.x % THREADS, group = threadIdx.x / THREADS;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64 % WAVES, at = threadIdx.x % THREADS;
+  const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS);
   const int64_t row = P.row0 + (int64_t)blockIdx.x * ROWS + group;
   if (row >= P.rows) return;  // (ROWS > 1: a wave to a row, nothing to wait for)
   float (*room[4])[2] = {&sums[0][group * WAVES], &sums[1][group * WAVES], &sums[2][group * WAVES], &sums[3][group * WAVES]};
   double *wide_room = &wide_sums[group * WAVES];
   auto column = [&](int u) { return 8 * (u * THREADS + at); };
-  const float over_cols = 1.0f / (float)(P.cols > 0 ? P.cols : 1);
+  auto there = [&](int c, int e) { return WHOLE || c + e < P.cols; };  // where c is
+  // eight numbers as they lie in memory: what is sent for ahead is not worked on, and so not waited for
+  auto raw = [&](const void *p, int64_t from, int c) -> Eight {
+    Eight x = {};
+    if (c >= P.cols) return x;
+    const T *q = static_cast<const T *>(p) + from + c;
+    if (WHOLE || c + 8 <= P.cols) return reinterpret_cast<const real_quad<Eight> *>(q)->v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (c + e < P.cols) x[e] = q[e];
+    return x;
+  };
+  const float columns = (float)(P.cols > 0 ? P.cols : 1);
 
+  Eight residual[HELD], gates[HELD];
+  const int64_t gate_row = P.gate ? row / P.gate_rows : 0;
+  auto ahead = [&]() {
+#pragma unroll
+    for (int u = 0; u < HELD; ++u) {
+      if (P.R) residual[u] = raw(P.R, row * P.ldr, column(u));
+      if (P.gate) gates[u] = raw(P.gate, gate_row * P.ldg, column(u));
+    }
+  };
   float v[HELD][8];
 #pragma unroll
   for (int u = 0; u < HELD; ++u)
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[u][e] = 0.0f;
-  for (int j = 0; j < P.parts; ++j) {
-    const int64_t place = P.places ? P.places[row * P.parts + j] : row * P.parts + j;
-    const float w = P.weights ? P.weights[row * P.parts + j] : 1.0f;
-    const bool there = place >= 0 && place < P.x_rows;
+  auto add = [&](const Eight (&x)[HELD], float w) {
 #pragma unroll
     for (int u = 0; u < HELD; ++u) {
-      const int c = column(u);
-      float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-      if (there && c < P.cols) load_part<T>(P.X, place * P.ldx + c, P.cols - c, x);
+      if (column(u) >= P.cols) continue;
+      const v8f f = __builtin_convertvector(x[u], v8f);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[u][e] = c + e < P.cols ? __builtin_fmaf(w, x[e], v[u][e]) : 0.0f;
+      for (int e = 0; e < 8; ++e) v[u][e] = there(column(u), e) ? __builtin_fmaf(w, f[e], v[u][e]) : 0.0f;
+    }
+  };
+  // Up to 64 parts at a time: their places and weights by the lanes in one load each, their rows four at a time.
+  for (int j0 = 0; j0 < P.parts; j0 += 64) {
+    const int here = P.parts - j0 < 64 ? P.parts - j0 : 64;
+    const int64_t j = row * P.parts + j0 + (lane < here ? lane : 0);
+    const int places = P.places ? P.places[j] : 0;
+    const float weights = P.weights ? P.weights[j] : 1.0f;
+    if (j0 == 0) ahead();
+    for (int i = 0; i < here; i += 4) {
+      Eight x[4][HELD];
+      float w[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        w[k] = 0.0f;
+        if (i + k >= here) continue;
+        const int64_t place = P.places ? __builtin_amdgcn_readlane(places, i + k) : row * P.parts + j0 + i + k;
+        w[k] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(weights), i + k));
+        const bool has = place >= 0 && place < P.x_rows;
+#pragma unroll
+        for (int u = 0; u < HELD; ++u) x[k][u] = raw(P.X, has ? place * P.ldx : 0, has ? column(u) : P.cols);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (i + k < here) add(x[k], w[k]);
     }
   }
 
@@ -118,37 +167,47 @@ __global__ __launch_bounds__(64 * WAVES *ROWS) void join_kernel(JoinArgs P) {
     double whole;
   };
   auto norm = [&](int kind, float (*room0)[2], float (*room1)[2]) -> Factor {
+    const bool layer = kind == ROW_NORM_LAYER;
     float mean = 0.0f;
-    if (kind == ROW_NORM_LAYER) {
-      TwoSums s{0.0f, 0.0f};
+    TwoSums s{0.0f, 0.0f};
+    if (layer) {
 #pragma unroll
       for (int u = 0; u < HELD; ++u)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s.a += v[u][e];
-      mean = row_sums<WAVES>(s, room0, wave, lane).a * over_cols;
-    }
-    TwoSums s{0.0f, 0.0f};
+        for (int e = 0; e < 8; ++e) s.b += v[u][e];
+      mean = __fdiv_rn(row_sums<WAVES>(s, false, room0, wave, lane).b, columns);
+      s.b = 0.0f;
 #pragma unroll
-    for (int u = 0; u < HELD; ++u)
+      for (int u = 0; u < HELD; ++u) {
+        if (column(u) >= P.cols) continue;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float d = column(u) + e < P.cols ? v[u][e] - mean : 0.0f;
-        s.a += d;
-        s.b = __builtin_fmaf(d, d, s.b);
+        for (int e = 0; e < 8; ++e) {
+          const float d = there(column(u), e) ? v[u][e] - mean : 0.0f;
+          s.a += d;
+          s.b = __builtin_fmaf(d, d, s.b);
+        }
       }
-    s = row_sums<WAVES>(s, room1, wave, lane);
-    const float rest = kind == ROW_NORM_LAYER ? s.a * over_cols : 0.0f;
-    const float square = __fdiv_rn(s.b, (float)(P.cols > 0 ? P.cols : 1)) - rest * rest + P.eps;
+    } else {
+#pragma unroll
+      for (int u = 0; u < HELD; ++u)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s.b = __builtin_fmaf(v[u][e], v[u][e], s.b);
+    }
+    s = row_sums<WAVES>(s, layer, room1, wave, lane);
+    const float rest = layer ? __fdiv_rn(s.a, columns) : 0.0f;
+    const float square = __fdiv_rn(s.b, columns) - rest * rest + P.eps;
     // (the same in the whole row; a deviation of a thousandth of the mean is left with too few bits)
     if (square >= 0x1p-100f && square <= 0x1p120f && square >= 0x1p-20f * mean * mean) {
+      if (layer) {
 #pragma unroll
-      for (int u = 0; u < HELD; ++u)
+        for (int u = 0; u < HELD; ++u)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[u][e] = kind == ROW_NORM_LAYER ? (v[u][e] - mean) - rest : v[u][e];
+          for (int e = 0; e < 8; ++e) v[u][e] = (v[u][e] - mean) - rest;
+      }
       return {__fdiv_rn(1.0f, __fsqrt_rn(square)), false, 0.0};
     }
     double m = 0.0, sum = 0.0;
-    if (kind == ROW_NORM_LAYER) {
+    if (layer) {
 #pragma unroll
       for (int u = 0; u < HELD; ++u)
 #pragma unroll
@@ -189,7 +248,7 @@ __global__ __launch_bounds__(64 * WAVES *ROWS) void join_kernel(JoinArgs P) {
         float x = v[u][e] * by;
         if (weight) x *= w[e];
         if (bias) x += b[e];
-        v[u][e] = c + e < P.cols ? x : 0.0f;
+        v[u][e] = there(c, e) ? x : 0.0f;
       }
     }
   };
@@ -198,26 +257,24 @@ __global__ __launch_bounds__(64 * WAVES *ROWS) void join_kernel(JoinArgs P) {
     weigh(P.post_weight, P.post_bias, f.by);
   }
 
-  const int64_t gate_row = P.gate ? row / P.gate_rows : 0;
 #pragma unroll
   for (int u = 0; u < HELD; ++u) {
     const int c = column(u);
     if (c >= P.cols) continue;
-    float x[8];
     if (P.gate) {
-      load_part<T>(P.gate, gate_row * P.ldg + c, P.cols - c, x);
+      const v8f g = __builtin_convertvector(gates[u], v8f);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[u][e] *= x[e];
+      for (int e = 0; e < 8; ++e) v[u][e] *= g[e];
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[u][e] *= P.scale;
     if (P.R) {
-      load_part<T>(P.R, row * P.ldr + c, P.cols - c, x);
+      const v8f r = __builtin_convertvector(residual[u], v8f);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[u][e] += x[e];
+      for (int e = 0; e < 8; ++e) v[u][e] += r[e];
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[u][e] = c + e < P.cols ? (float)(T)v[u][e] : 0.0f;
+    for (int e = 0; e < 8; ++e) v[u][e] = there(c, e) ? (float)(T)v[u][e] : 0.0f;
     if (P.H) store_part<T>(P.H, row * P.ldh + c, P.cols - c, v[u]);
   }
   if (!P.N && !P.Q) return;
@@ -256,20 +313,19 @@ __global__ __launch_bounds__(64 * WAVES *ROWS) void join_kernel(JoinArgs P) {
       for (int e = 0; e < 8; ++e) v[u][e] = P.norm_weight ? __fmul_rn(held[u][e], w[e]) : held[u][e];
     }
   }
-  float top = 0.0f, none = 0.0f;
+  float top = 0.0f, none = 0.0f;  // none: NaN where something is no number
 #pragma unroll
   for (int u = 0; u < HELD; ++u)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float z = column(u) + e < P.cols ? v[u][e] : 0.0f;
+      const float z = there(column(u), e) ? v[u][e] : 0.0f;
       none = __builtin_fmaf(z, 0.0f, none);
       top = __builtin_fmaxf(top, __builtin_fabsf(z));
     }
-  if (none != 0.0f) top = __builtin_nanf("");
-  auto larger = [](float a, float b) { return a != a ? a : (b <= a ? a : b); };
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) top = larger(top, __shfl_xor(top, d));
+  top = wave_most(top);
+  if (__ballot(none != 0.0f)) top = __builtin_nanf("");
   if constexpr (WAVES > 1) {
+    auto larger = [](float a, float b) { return a != a ? a : (b <= a ? a : b); };
     if (lane == 0) room[0][wave][0] = top;  // (every wave is behind the barrier of a later sum, or none was taken)
     __syncthreads();
     top = room[0][0][0];
@@ -290,17 +346,21 @@ __global__ __launch_bounds__(64 * WAVES *ROWS) void join_kernel(JoinArgs P) {
   }
 }
 
-template <typename T>
+template <typename T, bool WHOLE>
 hipError_t launch_for(const JoinArgs &P, hipStream_t s) {
   void (*kernel)(JoinArgs);
   unsigned threads = 256;
   int64_t rows = 1;
-  if (P.cols <= 512) { kernel = join_kernel<T, 1, 4, 1>; rows = 4; }
-  else if (P.cols <= 1024) { kernel = join_kernel<T, 1, 4, 2>; rows = 4; }
-  else if (P.cols <= 2048) kernel = join_kernel<T, 4, 1, 1>;
-  else if (P.cols <= 4096) kernel = join_kernel<T, 4, 1, 2>;
-  else if (P.cols <= 8192) { kernel = join_kernel<T, 8, 1, 2>; threads = 512; }
-  else { kernel = join_kernel<T, 16, 1, 2>; threads = 1024; }
+  // (few rows: as many waves to each as it can use)
+  const bool few = P.rows - P.row0 <= 2 * compute_units();
+  if (P.cols <= 512) { kernel = join_kernel<T, 1, 4, 1, WHOLE>; rows = 4; }
+  else if (P.cols <= 1024 && !few) { kernel = join_kernel<T, 1, 4, 2, WHOLE>; rows = 4; }
+  else if (P.cols <= 2048) kernel = join_kernel<T, 4, 1, 1, WHOLE>;
+  else if (P.cols <= 4096 && !few) kernel = join_kernel<T, 4, 1, 2, WHOLE>;
+  else if (P.cols <= 4096) { kernel = join_kernel<T, 8, 1, 1, WHOLE>; threads = 512; }
+  else if (P.cols <= 8192 && !few) { kernel = join_kernel<T, 8, 1, 2, WHOLE>; threads = 512; }
+  else if (P.cols <= 8192) { kernel = join_kernel<T, 16, 1, 1, WHOLE>; threads = 1024; }
+  else { kernel = join_kernel<T, 16, 1, 2, WHOLE>; threads = 1024; }
   return launch_with(reinterpret_cast<const void *>(kernel), dim3((unsigned)((P.rows - P.row0 + rows - 1) / rows)), threads, 0, s, &P);
 }
 
@@ -313,9 +373,10 @@ hipError_t launch_join(JoinArgs P, int type, hipStream_t s) {
   for (int64_t i = 0; i < rows; i += slab) {
     P.row0 = i;
     P.rows = rows - i < slab ? rows : i + slab;
-    const hipError_t e = type == REAL_F32    ? launch_for<float>(P, s)
-                         : type == REAL_BF16 ? launch_for<__bf16>(P, s)
-                                             : launch_for<_Float16>(P, s);
+    const bool whole = P.cols % 8 == 0;
+    const hipError_t e = type == REAL_F32    ? (whole ? launch_for<float, true>(P, s) : launch_for<float, false>(P, s))
+                         : type == REAL_BF16 ? (whole ? launch_for<__bf16, true>(P, s) : launch_for<__bf16, false>(P, s))
+                                             : (whole ? launch_for<_Float16, true>(P, s) : launch_for<_Float16, false>(P, s));
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
