@@ -227,7 +227,7 @@ __device__ __forceinline__ void route_token(const RouteArgs &P, int type, int64_
 }
 
 // ---- four tokens to a wave ----
-// A row of 16 lanes takes a token, lane q the experts PER q .. PER q + PER - 1: what is done once for a token, the steps of a
+// A row of 16 lanes takes a token, a lane PER of its experts: what is done once for a token, the steps of a
 // maximum above all, is done for four at a time.
 
 template <int BY>
@@ -282,17 +282,19 @@ __device__ __forceinline__ int larger_in_row(double v, int number) {
 }
 
 // Lane q < top (at most 15) gets its token's q-th expert (-1: none) and its weight; returns whether the token has to be done again, in float64.
-// With groups: one or more whole lanes to a group, 1, 2, 4 or 8.
+// P.span lanes to a group, a power of two; their experts are neighbours, and the last of a group's lanes may have fewer or none.
 template <int PER>
 __device__ __forceinline__ bool route_row(const RouteArgs &P, int type, int64_t token, int lane, int *id, float *weight) {
-  const int q = lane & 15, first = q * PER;
+  const int q = lane & 15, span = P.span, group = q / span, part = q % span * PER;
+  const int each = (int)P.each.d, first = group * each + part;
+  const int own_experts = group < P.groups ? (each - part < PER ? each - part : PER) : 0;  // (none, or below)
   const int64_t at = token * P.ldl + first;
   float x[PER], bias[PER];
   bool lost = false;
   float largest = NONE;
 #pragma unroll
   for (int i = 0; i < PER; i += 4) {
-    if (first + i + 4 <= P.experts) {
+    if (i + 4 <= own_experts) {
       const v4f four = load_real4(P.logits, at + i, type);
       const v4f more = P.bias ? load_real4(P.bias, first + i, REAL_F32) : v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -303,7 +305,7 @@ __device__ __forceinline__ bool route_row(const RouteArgs &P, int type, int64_t 
     } else {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const bool here = first + i + k < P.experts;
+        const bool here = i + k < own_experts;
         x[i + k] = here ? load_real(P.logits, at + i + k, type) : NONE;
         bias[i + k] = here && P.bias ? P.bias[first + i + k] : 0.0f;
       }
@@ -345,7 +347,6 @@ __device__ __forceinline__ bool route_row(const RouteArgs &P, int type, int64_t 
   lost = any_of_row(lost, lane);
   bool doubt = false;
   if (P.groups > 1) {
-    const int span = (int)P.each.d / PER, group = q / span;
     float one = c[0], two = NONE;
 #pragma unroll
     for (int i = 1; i < PER; ++i) {
@@ -616,15 +617,24 @@ hipError_t launch_route(RouteArgs P, int type, void *ws, hipStream_t s) {
     P.counts = static_cast<uint8_t *>(ws);
     P.ranks = P.counts + counts_bytes(P.tokens, P.experts);
   }
-  // Four tokens to a wave (517 tokens, 60 experts 7.6 -> 5.1 us, 8192 and 256 12.3 -> 7.8); up to 32 a token has a wave of its own, which is sooner done.
-  const int per = P.experts <= 64 ? 1 : P.experts <= 128 ? 2 : P.experts <= 256 ? 4 : P.experts <= 512 ? 8 : 16;
-  const int each = (int)P.each.d, span = each / (4 * per);
-  const bool four = P.tokens > TOKENS && per <= 4 && P.top <= 15 &&
-                    (P.groups == 1 || (each % (4 * per) == 0 && (span == 1 || span == 2 || span == 4 || span == 8)));
+  // Four tokens to a wave (517 tokens, 60 experts 7.6 -> 5.1 us, 8192 and 256 12.3 -> 7.8), where the groups fit 16 lanes; up to 32 tokens one
+  // has a wave of its own, which is sooner done.
+  int per = P.experts <= 64 ? 1 : P.experts <= 128 ? 2 : P.experts <= 256 ? 4 : P.experts <= 512 ? 8 : 16;
+  bool four = P.tokens > TOKENS && per <= 8 && P.top <= 15;
+  if (four) {
+    int in_rows = per;  // experts of a lane / 4
+    for (; in_rows <= 8; in_rows *= 2) {
+      P.span = P.groups == 1 ? 16 : 1;
+      while ((int64_t)P.span * 4 * in_rows < (int64_t)P.each.d) P.span *= 2;
+      if (P.span * P.groups <= 16) break;
+    }
+    four = in_rows <= 8;
+    if (four) per = in_rows;
+  }
   void (*kernel)(RouteArgs, int) = per == 1   ? (four ? route_kernel<1, true> : route_kernel<1, false>)
                                    : per == 2 ? (four ? route_kernel<2, true> : route_kernel<2, false>)
                                    : per == 4 ? (four ? route_kernel<4, true> : route_kernel<4, false>)
-                                   : per == 8 ? route_kernel<8, false> : route_kernel<16, false>;
+                                   : per == 8 ? (four ? route_kernel<8, true> : route_kernel<8, false>) : route_kernel<16, false>;
   void *list[] = {&P, &type};
   hipError_t e = hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3((unsigned)blocks), dim3(four ? 512 : THREADS), list, 0, s);
   if (e == hipSuccess && P.counts) {

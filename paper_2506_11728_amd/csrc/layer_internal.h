@@ -65,6 +65,7 @@ struct RouteArgs {
   int64_t ldl, tokens;
   int experts, top, groups, top_groups, best, normalise, sigmoid;
   Divisor each;  // experts of a group
+  int span;      // the launcher's own: lanes of a group
   float scale;
 };
 size_t route_scratch(int64_t tokens, int64_t experts, int64_t top);

@@ -44,6 +44,7 @@ int mipgemm_route(int64_t tokens, int64_t experts, int64_t top, const void *logi
   P.experts = (int)experts; P.top = (int)top; P.groups = (int)groups; P.top_groups = (int)top_groups; P.best = (int)group_best;
   P.normalise = normalise != 0; P.sigmoid = scoring == MIPGEMM_SIGMOID;
   P.each = mip::divisor(experts / groups, mip::MOST_EXPERTS);
+  P.span = 16;
   P.scale = scale;
   return static_cast<int>(mip::launch_route(P, type, workspace, static_cast<hipStream_t>(stream)));
 }
