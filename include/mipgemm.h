@@ -764,7 +764,7 @@ int mipgemm_attention_kv4(int64_t requests, int64_t q_heads, int64_t kv_heads, i
  *
  * logits are of `type`, tokens ldl elements apart; ids, weights and places hold `top` entries to a token.
  * With starts and more than 32 tokens, a workspace of
- * mipgemm_route_workspace_size bytes (16-byte aligned) is needed.  Argument numbers: tokens=1 (at most 2^26)
+ * mipgemm_route_workspace_size bytes (16-byte aligned) is needed, which no other call may use at the same time.  Argument numbers: tokens=1 (at most 2^26)
  * experts=2 (1 to 1024) top=3 (1 to 32) logits=4 ldl=5 type=6 bias=7 scoring=8 groups=9 (1 to 64, a
  * divisor of experts) top_groups=10 group_best=11 (no more than a group has) normalise=12 scale=13
  * (finite) ids=14 weights=15 starts=16 order=17 places=18 workspace=19 workspace_bytes=20

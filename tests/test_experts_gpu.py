@@ -207,6 +207,29 @@ def test_sums_wrap_as_the_products_do(gpu):
         assert (C == float(np.float32(k * 16384 - 2 ** 32))).all()
 
 
+@pytest.mark.parametrize("rows", [3, 300])
+def test_offsets_that_pass_31_and_32_bits(gpu, rows):
+    import torch
+    g = torch.Generator().manual_seed(4)
+    k, n = 128, 4096
+    small = torch.randint(-127, 128, (rows, k), generator=g, dtype=torch.int8)
+    weights = torch.randint(-127, 128, (2, n, k), generator=g, dtype=torch.int8)
+    want = torch.cat([small[:rows // 3].double() @ weights[0].double().T, small[rows // 3:].double() @ weights[1].double().T])
+    starts = torch.tensor([0, rows // 3, rows], dtype=torch.int32, device="cuda")
+    for lda, ldb, strideB in ((1 << 14, k, n * k), (1 << 15, k, n * k), (k, 800000, 800000 * n), (k, 1 << 20, n << 20), (k, k, 5 * (1 << 30))):
+        a_rows = 200000 if lda > k else rows  # 3.3 or 6.6 GB
+        A = torch.empty((a_rows, lda), dtype=torch.int8, device="cuda")
+        at = torch.arange(a_rows - rows, a_rows)
+        A[at.cuda(), :k] = small.cuda()
+        B = torch.empty(strideB + (n - 1) * ldb + k, dtype=torch.int8, device="cuda")
+        for e in range(2):
+            torch.as_strided(B, (n, k), (ldb, 1), e * strideB).copy_(weights[e])
+        C = torch.zeros((rows, n), device="cuda")
+        gpu.mipgemm_s8s8_experts(rows, 2, n, k, A, lda, a_rows, None, starts, at.to(torch.int32).cuda(), 1, B, ldb, strideB, None, None, 0, 0, C, n, F32)
+        assert torch.equal(C.double().cpu(), want), (lda, ldb, strideB)
+        del A, B
+
+
 def test_scales_that_are_no_numbers_stay_in_their_rows_and_columns(gpu):
     import torch
     for counts in ([3, 4], [150, 200]):
