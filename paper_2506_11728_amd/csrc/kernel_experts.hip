@@ -1,7 +1,8 @@
 // The experts' products of rows sorted by expert, for operands of any alignment and any k:
 //     C(p, j) = act(float(A(p) . B(e, j)) a_scale b_scale + bias)
-// 64 rows of one expert by 64 columns to a workgroup (with a gate 64 pairs of columns), k in blocks of 64 through registers
-// into LDS, two stages, v_mfma_i32_32x32x32_i8.
+// 64 MB rows of one expert by 128 rows of its weights (with a gate 64 of the gate's and 64 of the others) to a workgroup, k in blocks of 64
+// through registers into LDS, two stages, v_mfma_i32_32x32x32_i8.  What bounds it is the memory path, which takes an unaligned piece for two: 64 experts,
+// 512 rows each on average, 1024 pairs of columns of 2048 392 us, where rows that are aligned take 197 by direct loads.
 #include "experts.h"
 #include "dma_common.h"
 
@@ -9,29 +10,31 @@ namespace mip {
 
 namespace {
 
-constexpr int TM = 64, TN = 64, TK = 64;
+constexpr int TN = 128, TK = 64;  // rows of B, k of a block
 
 struct Params {
   ExpertsArgs X;
   int64_t slot0, column0;
 };
 
-template <int GATED>
+template <int GATED, int MB>
 __global__ __launch_bounds__(256) void experts_kernel(Params P) {
-  constexpr int BROWS = TN * (1 + GATED), STAGE = (TM + BROWS) * TK;
+  constexpr int TM = 64 * MB;
+  constexpr int OUT = GATED ? TN / 2 : TN, STAGE = (TM + TN) * TK;
   __shared__ __attribute__((aligned(16))) uint8_t lds[2 * STAGE];
   __shared__ float scales[TM];
   const ExpertsArgs &X = P.X;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const ExpertTile tile = expert_tile(X.starts, X.experts, X.rows, TM, P.slot0 + blockIdx.y, lane);
   if (tile.count == 0) return;
-  const int64_t n0 = P.column0 + (int64_t)blockIdx.x * TN;
+  const int64_t n0 = P.column0 + (int64_t)blockIdx.x * OUT;
   const int64_t outputs = GATED ? 2 * X.n : X.n;
   using SA = Stage<TM, true, TK>;
-  using SB = Stage<BROWS, true, TK>;
-  // this thread's pieces: one of A, one or two of B
-  const uint8_t *from[SA::PER_THREAD + SB::PER_THREAD];
-  int to[SA::PER_THREAD + SB::PER_THREAD], deep[SA::PER_THREAD + SB::PER_THREAD];
+  using SB = Stage<TN, true, TK>;
+  // this thread's pieces of A and of B
+  constexpr int PIECES = SA::PER_THREAD + SB::PER_THREAD;
+  const uint8_t *from[PIECES];
+  int to[PIECES], deep[PIECES];
 #pragma unroll
   for (int i = 0; i < SA::PER_THREAD; ++i) {
     int a, c;
@@ -46,14 +49,14 @@ __global__ __launch_bounds__(256) void experts_kernel(Params P) {
   for (int i = 0; i < SB::PER_THREAD; ++i) {
     int a, c;
     SB::chunk_of(i, tid, a, c);
-    int64_t column = n0 + a % TN;
+    // (with a gate, blocks of 32 of its columns and of the others in turn: a wave has both of a pair)
+    int64_t column = n0 + (GATED ? a / 64 * 32 + a % 32 : a);
     if (column > X.n - 1) column = X.n - 1;
-    if (GATED && a >= TN) column += X.n;
+    if (GATED && (a / 32) % 2) column += X.n;
     from[SA::PER_THREAD + i] = X.B + tile.e * X.strideB + column * X.ldb + 16 * c;
     to[SA::PER_THREAD + i] = TM * TK + SB::lds_offset(a, c);
     deep[SA::PER_THREAD + i] = 16 * c;
   }
-  constexpr int PIECES = SA::PER_THREAD + SB::PER_THREAD;
   v4i held[PIECES];
   auto load = [&](int64_t k0) {
 #pragma unroll
@@ -67,7 +70,7 @@ __global__ __launch_bounds__(256) void experts_kernel(Params P) {
     for (int i = 0; i < PIECES; ++i) *reinterpret_cast<v4i *>(lds + stage * STAGE + to[i]) = held[i];
   };
   const int wm = wave >> 1, wn = wave & 1;
-  v16i acc[1 + GATED] = {};
+  v16i acc[MB][2] = {};
   const int64_t blocks = (X.k + TK - 1) / TK;
   if (blocks > 0) {
     load(0);
@@ -80,52 +83,74 @@ __global__ __launch_bounds__(256) void experts_kernel(Params P) {
     const uint8_t *sa = lds + (t & 1) * STAGE, *sb = sa + TM * TK;
 #pragma unroll
     for (int ks = 0; ks < TK / 32; ++ks) {
-      const v4i a = SA::fragment(sa, wm * 32, ks, lane);
+      v4i a[MB], b[2];
 #pragma unroll
-      for (int g = 0; g <= GATED; ++g) {
-        const v4i b = SB::fragment(sb, g * TN + wn * 32, ks, lane);
-        acc[g] = __builtin_amdgcn_mfma_i32_32x32x32_i8(b, a, acc[g], 0, 0, 0);
-      }
+      for (int i = 0; i < MB; ++i) a[i] = SA::fragment(sa, wm * (TM / 2) + 32 * i, ks, lane);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) b[j] = SB::fragment(sb, wn * 64 + 32 * j, ks, lane);
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(b[j], a[i], acc[i][j], 0, 0, 0);
     }
     if (more) store((t + 1) & 1);
     __syncthreads();
   }
-  // lane l has row l % 32 of the wave's block and, of column group q, columns 8 q + 4 (l / 32) .. + 3
-  const int row = wm * 32 + (lane & 31);
-  if (row >= tile.count) return;
-  const float row_scale = scales[row];
-  const int64_t p = tile.first + row;
-  auto value = [&](int sum, int64_t column) {
-    const int64_t at = tile.e * outputs + column;
-    return linear_value(sum, row_scale, X.b_scales ? X.b_scales[at] : 1.0f, X.bias ? X.bias[at] : 0.0f);
-  };
-  auto activated = [&](float y) {
-    switch (activation_kind(X.act)) {
-      case 0: return Activate<0>::of(X.act)(y);
-      case 1: return Activate<1>::of(X.act)(y);
-      default: return Activate<2>::of(X.act)(y);
+  // lane l has row l % 32 of a block and, of its quarter q, columns 8 q + 4 (l / 32) .. + 3
+  const LinearArgs L{X.C, nullptr, X.ldc, 0, nullptr, X.b_scales ? X.b_scales + tile.e * outputs : nullptr,
+                     X.bias ? X.bias + tile.e * outputs : nullptr, X.act, X.type};
+  auto put = [&](auto act) {
+#pragma unroll
+    for (int i = 0; i < MB; ++i) {
+      const int row = wm * (TM / 2) + 32 * i + (lane & 31);
+      if (row >= tile.count) continue;
+      const float row_scale = scales[row];
+#pragma unroll
+      for (int j = 0; j < (GATED ? 1 : 2); ++j) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int64_t col = n0 + wn * (OUT / 2) + 32 * j + 8 * q + 4 * (lane >> 5), count = X.n - col;
+          if (count <= 0) continue;
+          const LinearColumns c = linear_columns(L, col, count);
+          v4f y;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = act(linear_value(acc[i][j][4 * q + e], row_scale, c.scale[e], c.bias[e]));
+          if (GATED) {
+            const LinearColumns up = linear_columns(L, X.n + col, count);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] *= linear_value(acc[i][1][4 * q + e], row_scale, up.scale[e], up.bias[e]);
+          }
+          const int64_t at = (tile.first + row) * X.ldc + col;
+          if (count >= 4) {
+            store_real4<false>(X.C, at, X.type, y);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+              if (e < count) store_real(X.C, at + e, X.type, y[e]);
+          }
+        }
+      }
     }
   };
-#pragma unroll
-  for (int q = 0; q < 16; ++q) {
-    const int64_t j = n0 + wn * 32 + 8 * (q / 4) + 4 * (lane >> 5) + q % 4;
-    if (j >= X.n) continue;
-    float y = activated(value(acc[0][q], j));
-    if (GATED) y *= value(acc[GATED][q], X.n + j);
-    store_real(X.C, p * X.ldc + j, X.type, y);
+  switch (activation_kind(X.act)) {  // wave-uniform
+    case 0: put(Activate<0>::of(X.act)); break;
+    case 1: put(Activate<1>::of(X.act)); break;
+    default: put(Activate<2>::of(X.act)); break;
   }
 }
 
+template <int MB>
 hipError_t launch_unaligned(const ExpertsArgs &X, hipStream_t s) {
+  constexpr int TM = 64 * MB;
   // as many pieces as the experts' rows can be cut into; a grid has at most 65535 rows, and 2^32 - 1 threads a dimension
   const int64_t slots = X.rows / TM + (X.experts < X.rows ? X.experts : X.rows);
-  const int64_t columns = (X.n + TN - 1) / TN;
+  const int64_t out = X.gated ? TN / 2 : TN, columns = (X.n + out - 1) / out;
   constexpr int64_t MOST_X = 1 << 20, MOST_Y = 65535;
   for (int64_t c = 0; c < columns; c += MOST_X)
     for (int64_t slot = 0; slot < slots; slot += MOST_Y) {
-      Params P{X, slot, c * TN};
+      Params P{X, slot, c * out};
       const dim3 grid((unsigned)(columns - c < MOST_X ? columns - c : MOST_X), (unsigned)(slots - slot < MOST_Y ? slots - slot : MOST_Y));
-      const hipError_t e = launch_with(X.gated ? reinterpret_cast<const void *>(experts_kernel<1>) : reinterpret_cast<const void *>(experts_kernel<0>),
+      const hipError_t e = launch_with(X.gated ? reinterpret_cast<const void *>(experts_kernel<1, MB>) : reinterpret_cast<const void *>(experts_kernel<0, MB>),
                                        grid, 256, 0, s, &P);
       if (e != hipSuccess) return e;
     }
@@ -141,9 +166,10 @@ hipError_t launch_unaligned(const ExpertsArgs &X, hipStream_t s) {
 // unit, so that one's first loads and write-back go on beside the other's products; under a long k of many rows 192 x 256, which load less for a product (8 experts,
 // 512 rows each on average, 4096 columns of 11008: 221 us against 239; 1024 pairs of columns of 2048, 64 experts: 222 against 201).
 hipError_t launch_experts(const ExpertsArgs &X, hipStream_t s) {
-  if ((X.rows <= 12 * X.experts || experts_slim_tiles(X) <= 1024) && experts_slim_eligible(X)) return launch_experts_slim(X, s);
-  if (experts_tile_eligible(X)) return launch_experts_tile(X, X.k >= 4096 && X.rows >= 384 * X.experts, s);
-  return launch_unaligned(X, s);
+  const bool tiles = experts_tile_eligible(X);
+  if ((X.rows <= 12 * (int64_t)X.experts || experts_slim_tiles(X) <= 1024) && experts_slim_eligible(X)) return launch_experts_slim(X, s);
+  if (tiles) return launch_experts_tile(X, X.k >= 4096 && X.rows >= 384 * (int64_t)X.experts, s);
+  return X.rows <= 64 * (int64_t)X.experts ? launch_unaligned<1>(X, s) : launch_unaligned<2>(X, s);
 }
 
 }  // namespace mip
