@@ -3,7 +3,8 @@
 //
 // The time is that of reading the weights, so what counts is how many loads are on their way: both operands go from memory into
 // registers as v_mfma_i32_16x16x64_i8 takes them (16 rows x 64 bytes to a load), a block ahead, with no barrier before the four
-// sums are added up.  Rows of any alignment, any k.
+// sums are added up.  Rows of any alignment, any k.  One token, eight experts' 1024 pairs of columns of 2048 (34 MB): 9.4 us, where 256
+// rows of weights to a workgroup took 20; 256 rows over 64 experts' 2048 columns of 1024 (136 MB) 29.7 us, 4.6 TB/s.
 #include "dma_common.h"
 #include "epilogue16.h"
 #include "experts.h"
