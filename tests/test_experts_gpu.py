@@ -1,4 +1,6 @@
 """mipgemm_s8s8_experts against its definition in 64 bits."""
+import re
+
 import numpy as np
 import pytest
 
@@ -266,6 +268,167 @@ def test_experts_in_a_graph_and_on_another_stream(gpu):
         A.copy_(torch.randint(-127, 128, (tokens, k), generator=g, dtype=torch.int8))
         starts.copy_(torch.tensor([0] + list(_counts(experts, tokens * top - 20 * i, i, 0.6))).cumsum(0))
         order.copy_(torch.randperm(tokens * top, generator=g))
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got, eager = out.clone(), torch.zeros_like(out)
+        call(eager)
+        torch.cuda.synchronize()
+        assert torch.equal(got, eager), i
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            call(eager.zero_())
+        side.synchronize()
+        assert torch.equal(got, eager), i
+
+
+# ---- the kernels for many rows, by name: sizes that the kernel of 16 rows to a workgroup leaves to them ----
+
+def _served(kernels_of, gpu, case):
+    """The kernel that serves a case, with its template's arguments."""
+    names = [re.search(r"experts_\w*kernel<[^>]*>", n) for n in kernels_of(lambda: case.call(gpu))]
+    names = [n.group(0) for n in names if n]
+    assert len(names) == 1, names
+    return names[0]
+
+
+RAGGED = [129, 1, 0, 257]                 # experts whose rows end inside tiles of 128
+FEW = [40, 13, 64, 0, 1, 65, 20, 33]      # 13 to 64 rows to an expert on average
+LONG = [700, 70]                          # at least 384, over a k of 4096 and more
+
+
+@pytest.mark.parametrize("k", [16, 112, 128, 144, 256, 272, 400])
+@pytest.mark.parametrize("gated", [False, True])
+def test_tiles_of_many_rows(gpu, kernels_of, k, gated):
+    """One block of k, several, and what is left of it; columns that end inside a tile, at its end and one behind it."""
+    for i, n in enumerate((1250, 1280, 1217) if gated else (2501, 2560, 2433)):
+        for pad in (0, 16):
+            j = i + k // 16 + pad // 16
+            case = Case(RAGGED, n, k, top=1 + j % 3, gated=gated, gather=j % 2 == 0, pad=pad, kind=j % 3, act=j % 5, bias=j % 4 > 0, seed=j)
+            if i == 0:
+                assert _served(kernels_of, gpu, case) == "experts_tile_kernel<128, 128, %d>" % gated
+            case.check(gpu)
+
+
+@pytest.mark.parametrize("act", [NONE, RELU, GELU, GELU_TANH, SILU])
+@pytest.mark.parametrize("gated", [False, True])
+def test_tiles_in_every_type_and_activation(gpu, act, gated):
+    for kind in (F32, BF16, F16):
+        Case([128, 300, 2, 31], 1251 if gated else 2500, 208, gated=gated, kind=kind, act=act, seed=act, gather=kind != F16).check(gpu)
+        Case([128, 300, 2, 31], 1251 if gated else 2500, 208, gated=gated, kind=kind, act=act, seed=act, scales=False, bias=kind == F32, behind=0).check(gpu)
+
+
+@pytest.mark.parametrize("k", [4096, 4112, 4208])
+@pytest.mark.parametrize("gated", [False, True])
+def test_large_tiles_under_a_long_sum(gpu, kernels_of, k, gated):
+    for i, (counts, n) in enumerate([(LONG, 700), ([384, 0, 769], 640), ([385], 1281)] if gated else [(LONG, 1345), ([384, 0, 769], 1280), ([385], 2561)]):
+        j = i + k // 16 + gated
+        case = Case(counts, n, k, top=1 + j % 2, gated=gated, gather=j % 2 == 0, pad=16 * (i % 2), kind=j % 3, act=(NONE, SILU, GELU)[j % 3],
+                    bias=i > 0, seed=j)
+        assert _served(kernels_of, gpu, case) == "experts_tile_kernel<192, 256, %d>" % gated
+        case.check(gpu)
+
+
+@pytest.mark.parametrize("counts,blocks", [(FEW, 1), (RAGGED, 2)])
+@pytest.mark.parametrize("k", [1, 15, 17, 63, 65, 100, 130, 200])
+@pytest.mark.parametrize("gated", [False, True])
+def test_unaligned_rows_of_many(gpu, kernels_of, counts, blocks, k, gated):
+    for i, n in enumerate((1601, 1664) if gated else (3101, 3200)):
+        for pad in (0, 3):
+            j = i + k + pad
+            case = Case(counts, n, k, top=1 + j % 3, gated=gated, gather=j % 2 == 0, pad=pad, kind=j % 3, act=(j // 2) % 5, bias=j % 4 > 0, seed=j)
+            if i == 0 and pad == 0:
+                assert _served(kernels_of, gpu, case) == "experts_kernel<%d, %d>" % (gated, blocks)
+            case.check(gpu)
+
+
+@pytest.mark.parametrize("counts,blocks", [(FEW, 1), (RAGGED, 2)])
+@pytest.mark.parametrize("shift,pad", [(1, 0), (8, 0), (4, 16), (0, 8)])
+def test_unaligned_places_of_many_rows(gpu, kernels_of, counts, blocks, shift, pad):
+    for gated in (False, True):
+        case = Case(counts, 1601 if gated else 3101, 192, gated=gated, kind=BF16 if gated else F32, act=SILU, pad=pad, shift=shift, seed=shift + pad)
+        assert _served(kernels_of, gpu, case) == "experts_kernel<%d, %d>" % (gated, blocks)
+        case.check(gpu)
+
+
+# what each kernel for many rows is called with: rows of the experts, columns, k, padding
+MANY = [(RAGGED, 2501, 272, 0), (LONG, 1345, 4112, 0), (FEW, 3101, 130, 0), (RAGGED, 2501, 200, 3)]
+
+
+@pytest.mark.parametrize("counts,n,k,pad", MANY)
+def test_rows_that_a_does_not_have_among_many(gpu, counts, n, k, pad):
+    for gated in (False, True):
+        c = Case(counts, n, k, top=3, pad=pad, gated=gated, kind=F32 if gated else BF16, act=SILU)
+        c.order[1], c.order[5], c.order[20], c.order[40], c.order[131] = -1, c.a_rows * 3, 2 ** 31 - 1, -2 ** 31, -7
+        c.check(gpu)
+
+
+@pytest.mark.parametrize("counts,n,k,pad", MANY)
+def test_starts_of_many_rows_beyond_the_bound_and_out_of_order(gpu, counts, n, k, pad):
+    import torch
+    c = Case(counts, n, k, kind=F32, behind=0, gather=False, pad=pad)
+    whole, used = c.call(gpu).clone(), c.used
+    fine = c.starts.clone()
+    c.starts = fine.clone()
+    c.starts[-1] = 2 ** 31 - 1
+    assert torch.equal(c.call(gpu, bound=2)[:used], whole)
+    for at, to in ((0, -9), (0, 100), (1, 2 ** 31 - 1), (1, -2 ** 31), (-1, 50)):
+        c.starts = fine.clone()
+        c.starts[at] = to
+        got = c.call(gpu, bound=2)
+        assert (got[used:] == 3).all()
+        if to == -9:
+            assert torch.equal(got[:used], whole)
+
+
+@pytest.mark.parametrize("counts,n,k,pad", MANY)
+def test_scales_of_many_rows_that_are_no_numbers(gpu, counts, n, k, pad):
+    import torch
+    c = Case(counts, n, k, kind=F32, bias=False, gather=False, pad=pad)
+    last = max(e for e, rows in enumerate(counts) if rows)
+    c.a[1], c.b[last, 7], c.b[last, n - 1] = float("nan"), float("inf"), float("nan")
+    got = c.call(gpu).cpu()
+    bad = torch.zeros((c.used, n), dtype=torch.bool)
+    bad[1] = True
+    bad[c.used - counts[last]:, 7] = bad[c.used - counts[last]:, n - 1] = True
+    assert torch.equal(~torch.isfinite(got[:c.used, :n]), bad)
+
+
+@pytest.mark.parametrize("rows,n,pad", [(300, 3500, 0), (400, 2600, 0), (300, 3500, 1), (50, 16400, 1)])
+def test_sums_of_many_rows_wrap_as_the_products_do(gpu, rows, n, pad):
+    import torch
+    k = 140032  # 140032 * 2^14 is past 2^31
+    A = torch.full((rows, k + pad), -128, dtype=torch.int8, device="cuda")
+    B = torch.full((1, n, k + pad), -128, dtype=torch.int8, device="cuda")
+    C = torch.zeros((rows, n), device="cuda")
+    starts = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    gpu.mipgemm_s8s8_experts(rows, 1, n, k, A, k + pad, rows, None, starts, None, 1, B, k + pad, n * (k + pad), None, None, 0, 0, C, n, F32)
+    assert (C == float(np.float32(k * 16384 - 2 ** 32))).all()
+
+
+@pytest.mark.parametrize("counts,n,k,pad", MANY)
+def test_many_rows_in_a_graph(gpu, counts, n, k, pad):
+    """Captured once, replayed over other rows of the experts and other codes, against eager calls."""
+    import torch
+    c = Case(counts, n, k, top=1, kind=BF16, act=RELU, pad=pad)
+    g = torch.Generator().manual_seed(3)
+    lead, rows = k + pad, c.rows
+    A, B = c.A.cuda(), c.B.cuda()
+    a, b, bias, starts, order = (x.cuda() for x in (c.a, c.b, c.bias, c.starts, c.order))
+    out = torch.zeros((rows, n), dtype=torch.bfloat16, device="cuda")
+
+    def call(C):
+        gpu.mipgemm_s8s8_experts(rows, c.experts, n, k, A, lead, c.a_rows, a, starts, order, 1, B, lead, n * lead, b, bias, RELU, 0, C, n, BF16)
+    call(out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out)
+    for i in range(4):
+        A.copy_(torch.randint(-127, 128, A.shape, generator=g, dtype=torch.int8))
+        starts.copy_(torch.tensor([0] + list(_counts(c.experts, rows - 30 * i, i, 0.6))).cumsum(0))
+        order.copy_(torch.randperm(c.a_rows, generator=g)[:rows])
         out.zero_()
         graph.replay()
         torch.cuda.synchronize()
