@@ -1,4 +1,6 @@
 """mipgemm_join_rows against its definition in 64 bits."""
+import re
+
 import numpy as np
 import pytest
 
@@ -298,3 +300,69 @@ def test_join_in_a_graph_and_on_another_stream(gpu):
             call(again)
         side.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, again)), i
+
+
+# ---- the forms for more rows than two to a compute unit, whose threads keep more of a row ----
+
+MANY = [(513, 513, "1, 4, 2, false"), (520, 520, "1, 4, 2, true"), (600, 1024, "1, 4, 2, true"), (530, 1025, "4, 1, 1, false"),
+        (530, 2050, "4, 1, 2, false"), (520, 2056, "4, 1, 2, true"), (600, 4096, "4, 1, 2, true"), (515, 4099, "8, 1, 2, false"),
+        (515, 4100, "8, 1, 2, false"), (513, 8184, "8, 1, 2, true"), (514, 8192, "8, 1, 2, true"), (513, 8193, "16, 1, 2, false")]
+
+
+def _served(kernels_of, gpu, case):
+    """The kernel that serves a case of float32, with its template's arguments."""
+    names = [re.search(r"join_kernel<([^>]*)>", n) for n in kernels_of(lambda: case.call(gpu))]
+    names = [n.group(1) for n in names if n]
+    assert len(names) == 1, names
+    return names[0]
+
+
+@pytest.mark.parametrize("rows,cols,form", MANY)
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+def test_many_rows(gpu, kernels_of, rows, cols, form, kind):
+    i = MANY.index((rows, cols, form)) + kind
+    first = Case(rows, cols, (1, 2, 3)[i % 3], kind, RMS, RMS, gate_rows=(200, 0, rows, 1)[i % 4], scale=0.22, pad=(0, 3, 8)[i % 3], seed=i)
+    if kind == F32:
+        assert _served(kernels_of, gpu, first) == "float, " + form
+    first.check(gpu, in_place=i % 2 == 0)
+    Case(rows, cols, (2, 1)[i % 2], kind, LAYER, LAYER, gate_rows=(0, 7)[i % 2], biases=True, pad=(5, 0)[i % 2], residual=i % 3 > 0, seed=i + 1).check(gpu)
+    Case(rows, cols, 1, kind, NO, (RMS, LAYER, NO)[i % 3], weights=i % 2 == 0, shuffled=i % 4 > 0, seed=i + 2).check(gpu, in_place=True)
+
+
+@pytest.mark.parametrize("cols", [520, 1001, 2056, 4096, 4100, 8192])
+def test_many_rows_that_are_no_numbers_and_of_extreme_size(gpu, cols):
+    import torch
+    rows = 520
+    by = torch.tensor([1, 1e17, 1e19, 1e30, 1e35, 1e-17, 1e-20, 1e-25, 1e-30, 1e-34], dtype=torch.float64).repeat(52)
+    for kind, post, norm in ((F32, NO, RMS), (BF16, NO, LAYER), (F32, LAYER, NO)):
+        case = Case(rows, cols, 1, kind, post, norm, residual=False, shuffled=False, eps=1e-12, seed=15)
+        case.X = (torch.randn((rows, cols), generator=torch.Generator().manual_seed(16), dtype=torch.float64) * by[:, None]).to(R.TORCH[kind])
+        case.check(gpu)
+        clean = case.call(gpu)
+        case.X[1, cols // 2], case.X[300, 0], case.X[519, cols - 1] = float("nan"), float("inf"), -float("inf")
+        H, N, Q, s = case.call(gpu)
+        others = torch.ones(rows, dtype=torch.bool)
+        others[[1, 300, 519]] = False
+        for r in (1, 300, 519):
+            assert not torch.isfinite(N[r]).all() and torch.isnan(s[r]) and (Q[r, :cols] == 0).all()
+        for a, b in zip((H, N, Q, s[:-1]), clean):
+            assert torch.equal(a.cpu()[others], b.cpu()[:rows][others])
+
+
+@pytest.mark.parametrize("parts", [63, 64, 65, 130, 1024])
+@pytest.mark.parametrize("rows,cols", [(3, 100), (2, 1500), (1, 4096)])
+def test_many_parts(gpu, parts, rows, cols):
+    """More parts than a wave has lanes, with places and weights, without either, and without both."""
+    import torch
+    for shuffled in (True, False):
+        for weights in (True, False):
+            case = Case(rows, cols, parts, BF16 if weights else F32, NO, RMS, shuffled=shuffled, pad=3, seed=parts)
+            if not weights:
+                case.w = None
+            case.check(gpu)
+            if shuffled:
+                case.places[0, 0], case.places[-1, parts - 1], case.places[0, min(64, parts - 1)] = -1, -3, rows * parts
+                case.check(gpu)
+                if weights:
+                    case.w[-1, parts - 1] = float("nan")
+                    assert torch.isnan(case.call(gpu)[0][-1, :cols]).all()
