@@ -343,7 +343,8 @@ __global__ __launch_bounds__(64 * WAVES *ROWS) void join_kernel(JoinArgs P) {
   }
   if (at == 0) {
     float scale = finite ? __fdiv_rn(top, 127.0f) : __builtin_nanf("");
-    if (apart && top != 0.0f) scale = f.wide ? (float)((double)scale * f.whole) : scale * f.by;
+    // (a 127th of the smallest numbers has few bits left, so what goes through float64 does so from the largest on)
+    if (apart && finite && top != 0.0f) scale = f.wide ? (float)((double)top * f.whole / 127.0) : scale * f.by;
     P.scales[row] = scale;
   }
 }

@@ -366,3 +366,26 @@ def test_many_parts(gpu, parts, rows, cols):
                 if weights:
                     case.w[-1, parts - 1] = float("nan")
                     assert torch.isnan(case.call(gpu)[0][-1, :cols]).all()
+
+
+@pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("cols", [96, 1500, 4096])
+@pytest.mark.parametrize("rows", [8, 520])
+def test_scales_of_rows_next_to_the_smallest_numbers(gpu, kind, cols, rows):
+    """A 127th of a row's largest has few bits left below 2^-126; what the norm makes of it has all of them."""
+    import torch
+    by = torch.tensor([1e-36, 1e-37, 1e-38, 1e-39, 1e-40, 1e-41, 1e-42, 1e-43], dtype=torch.float64).repeat(rows // 8)
+    case = Case(rows, cols, 1, kind, NO, RMS, residual=False, shuffled=False, weights=False, eps=0.0, seed=17)
+    case.X = (torch.randn((rows, cols), generator=torch.Generator().manual_seed(18), dtype=torch.float64) * by[:, None]).to(R.TORCH[kind])
+    H, N, Q, s = case.call(gpu)
+    assert torch.equal(H.cpu(), case.X)
+    x = case.X.double()
+    z = (x / torch.sqrt((x * x).mean(1, keepdim=True))).nan_to_num(0.0)  # (rows that bfloat16 has only zeros for stay zeros)
+    assert ((N.double().cpu() - z).abs() <= 60 * U * z.abs() + R.rounding(z, kind)).all()
+    # the factor and the product are in float64: one rounding to float32 is left (U), and there is room for two more
+    assert ((s[:-1].double().cpu() - z.abs().amax(1) / 127).abs() <= 3 * U * z.abs().amax(1) / 127).all()
+    q, other = torch.empty_like(Q), torch.empty_like(s)
+    gpu.mipgemm_quantize_rows(rows, cols, H, cols, kind, torch.ones(cols, device="cuda"), 0.0, q, cols + 1, other)
+    torch.cuda.synchronize()
+    assert torch.equal(q[:, :cols], Q[:, :cols])
+    assert ((other[:-1].double() - s[:-1].double()).abs() <= 60 * U * s[:-1]).all()
