@@ -56,6 +56,15 @@ __device__ __forceinline__ double wave_sum(double v) {
 
 constexpr float NONE = -__builtin_inff();
 
+// The score of a chosen expert that is divided by the sum of them all or, where the chosen are, of theirs: softmax without its denominator, and for
+// weights that add up to one times a power of e, the same for the whole token, that leaves the largest of the chosen (of logit `top`) at 1 / 2 or more.
+// So float32 holds, of shares of 2^-126 and more, all bits: a sigmoid is e^l / (1 + e^l) below zero, and times e^-top there e^(l - top) / (1 + e^l).
+__device__ __forceinline__ float to_weigh(const RouteArgs &P, float logit, float top, float largest) {
+  if (!P.sigmoid) return expf(logit - (P.normalise ? top : largest));
+  const float from = P.normalise ? __builtin_fminf(top, 0.0f) : 0.0f;
+  return __fdiv_rn(logit < 0.0f ? expf(logit - from) : 1.0f, 1.0f + expf(-__builtin_fabsf(logit)));
+}
+
 // What a wave knows of its token's choice: lane j holds the j-th.
 struct Chosen {
   int id, count;  // count: how many there are (the same in every lane)
@@ -213,12 +222,7 @@ __device__ __forceinline__ void route_token(const RouteArgs &P, int type, int64_
     w = __builtin_nanf("");
   } else if (chosen.count > 0) {
     const float top = wave_most(any ? chosen.logit : NONE);
-    // (far below zero the sigmoid is its exponential to the last bit of a float64, and may pass float32)
-    const bool ratio = P.normalise && (!P.sigmoid || top < -40.0f);
-    float s;
-    if (P.sigmoid && !ratio) s = chosen.logit < -40.0f ? expf(chosen.logit) : __fdiv_rn(1.0f, 1.0f + expf(-chosen.logit));
-    else s = expf(chosen.logit - (ratio ? top : largest));
-    if (!any) s = 0.0f;
+    const float s = any ? to_weigh(P, chosen.logit, top, largest) : 0.0f;
     const float over = P.normalise ? wave_sum(s) : (P.sigmoid ? 1.0f : all);
     w = any ? P.scale * __fdiv_rn(s, over) : 0.0f;
   }
@@ -427,11 +431,7 @@ __device__ __forceinline__ bool route_row(const RouteArgs &P, int type, int64_t 
   const bool any = mine >= 0;
   const float logit = any ? load_real(P.logits, token * P.ldl + mine, type) : NONE;
   const float top = row_most(logit);
-  const bool ratio = P.normalise && (!P.sigmoid || top < -40.0f);
-  float s;
-  if (P.sigmoid && !ratio) s = logit < -40.0f ? expf(logit) : __fdiv_rn(1.0f, 1.0f + expf(-logit));
-  else s = expf(logit - (ratio ? top : largest));
-  if (!any) s = 0.0f;
+  const float s = any ? to_weigh(P, logit, top, largest) : 0.0f;
   const float over = P.normalise ? row_sum(s) : (P.sigmoid ? 1.0f : all);
   *id = mine;
   *weight = lost ? __builtin_nanf("") : (any ? P.scale * __fdiv_rn(s, over) : 0.0f);

@@ -286,3 +286,21 @@ def test_routing_in_a_graph_and_on_another_stream(gpu):
             route(again)
         side.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, again)), i
+
+
+@pytest.mark.parametrize("tokens", [5, 70])
+@pytest.mark.parametrize("experts", [8, 300, 600])
+def test_weights_far_below_the_largest(gpu, tokens, experts):
+    """Sigmoid scores that float32 does not hold, whose shares of a sum as small it does."""
+    import torch
+    x = torch.full((tokens, experts), -200.0)
+    x[:, :6] = torch.tensor([-36.0, -39.5, -88.0, -96.5, -103.0, -110.0])
+    x = x - 0.05 * torch.arange(tokens)[:, None] % 3
+    x[1::5, 0] = 0.3
+    x[2::5, 0] = -0.25
+    x[3::5, 0] = -41.0
+    x[4::5, :2] = -70.0
+    for normalise in (True, False):
+        _check(gpu, x, F32, 6, sigmoid=True, normalise=normalise)
+        _check(gpu, x, F32, 6, sigmoid=True, normalise=normalise, bias=torch.zeros(experts))
+        _check(gpu, x, F32, 6, sigmoid=True, normalise=normalise, groups=2, top_groups=2, best=2, scale=2.5)
