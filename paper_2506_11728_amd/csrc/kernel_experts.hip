@@ -1,8 +1,9 @@
 // The experts' products of rows sorted by expert, for operands of any alignment and any k:
 //     C(p, j) = act(float(A(p) . B(e, j)) a_scale b_scale + bias)
 // 64 MB rows of one expert by 128 rows of its weights (with a gate 64 of the gate's and 64 of the others) to a workgroup, k in blocks of 64
-// through registers into LDS, two stages, v_mfma_i32_32x32x32_i8.  What bounds it is the memory path, which takes an unaligned piece for two: 64 experts,
-// 512 rows each on average, 1024 pairs of columns of 2048 392 us, where rows that are aligned take 197 by direct loads.
+// through registers into LDS, two stages, v_mfma_i32_32x32x32_i8.  64 experts, 512 rows each on average, 1024 pairs of columns of 2048: 400 us, where rows that
+// are aligned take 196 by direct loads.  A wave waits for 76 % of its life, the matrix units are busy for 16 % of the time: the loads bound it, 11 bytes
+// a clock to a compute unit in unaligned pieces of 16; where k is no multiple of 16 the last piece of a row comes byte by byte.
 #include "experts.h"
 #include "dma_common.h"
 
@@ -164,7 +165,10 @@ hipError_t launch_unaligned(const ExpertsArgs &X, hipStream_t s) {
 // pairs of columns of 2048, 8 rows each on average 57.3 us, with tiles 63.2; 12 rows 61.9 and 60.0; 16 rows 69.7 and 63.5; 8 experts' 4096 columns of 4096,
 // 16 rows each 36.7 and 39.2, 32 rows 49.7 and 40.0).  Else tiles of rows that can be streamed: 128 x 128, two workgroups to a compute
 // unit, so that one's first loads and write-back go on beside the other's products; under a long k of many rows 192 x 256, which load less for a product (8 experts,
-// 512 rows each on average, 4096 columns of 11008: 221 us against 239; 1024 pairs of columns of 2048, 64 experts: 222 against 201).
+// 512 rows each on average, 4096 columns of 11008: 216 us against 243; 5504: 124 and 126; 4096: 100 and 98; 2048: 62 and 54; 64 experts, 512 rows each,
+// 1024 pairs of columns of 2048: 222 and 201).  The rule counts neither the columns nor the rounds of workgroups on the compute units, which decide
+// where there are few: 384 rows each under 11008 take 216 with the large tiles and 190 with the small ones, 256 rows 128 and 165; 512 rows and 1024
+// columns 98 and 82, under 4096 42 and 31.
 hipError_t launch_experts(const ExpertsArgs &X, hipStream_t s) {
   const bool tiles = experts_tile_eligible(X);
   if ((X.rows <= 12 * (int64_t)X.experts || experts_slim_tiles(X) <= 1024) && experts_slim_eligible(X)) return launch_experts_slim(X, s);

@@ -5,6 +5,9 @@
 // and three for B, the four waves 2 x 2 over the tile, v_mfma_i32_16x16x64_i8 with direct loads and fragment reads between
 // them.  A direct load takes its address by lane, so that gathered rows cost nothing over neighbouring ones.
 //
+// 64 experts, 512 rows each on average, 1024 pairs of columns of 2048: 196 us, matrix units busy for 34 % of the time; 8 experts, 512 rows each, 4096
+// columns of 11008: 216 us, 45 % (62 % of the time in which a compute unit has a tile: two rounds that fill one and a half).
+//
 // With a gate, blocks of 16 of its columns and 16 of the others take turns in LDS, so that a lane has the sums of a pair in
 // two of its accumulators.
 #include "dma_k128.h"

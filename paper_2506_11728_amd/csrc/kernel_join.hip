@@ -2,8 +2,9 @@
 //     y = sum_j w_j X(place_j),  u = norm(y),  H = R + scale gate u,  z = norm(H),  N = z,  Q = rint(127 z / max |z|).
 // A row stays in the registers of its workgroup throughout: X, R and the gate are read once and H, N and Q written once, so
 // memory bounds it; the norms' weights, the same for every row, come from the caches.  8192 rows of 4096 in bfloat16 between two RMS norms,
-// gated: 71 us (3.8 TB/s; 103 with residual and gate loaded behind the first norm, elements masked one by one and sums by shuffles), 8192 rows of
-// eight parts of 2048 79 us (4.7 TB/s); one row of eight parts of 4096 6 us.
+// gated: 71 us (3.8 TB/s; vector instructions issue for 43 of them; into codes in place of values 82 and 58; 103 with residual and gate loaded behind
+// the first norm, elements masked one by one and sums by shuffles), 8192 rows of eight parts of 2048 79 us (4.7 TB/s); one row of eight parts of 4096
+// 6 us, of one part 5.
 //
 // A mean is subtracted in two steps: the sum of what is left after the first is taken along with the sum of squares, so
 // that numbers far from zero keep their differences.  Sums of squares that float32 does not hold are taken again in

@@ -1,12 +1,17 @@
 // Routing of tokens to experts, and the tokens' rows sorted by expert.
 //
-// A wave takes a token, its lanes the experts 64 i + lane.  What is compared:
+// Up to 32 tokens a wave takes a token, its lanes the experts 64 i + lane (route_token); of more a row of 16 lanes takes one, four to a wave, where
+// 16 lanes hold the groups, of up to 512 experts with up to 15 chosen (route_row).  What is compared:
 //   the logits themselves where nothing is added to the scores and no sum of two of them is asked for: softmax and the
 //   sigmoid rise with the logit, so the order of the exact scores is that of the logits, and it is exact;
 //   else c = score + bias in float32.  Each is off by at most `wrong`; where two that are compared, of neighbours in
 //   the order, or of the last group that stays and the first that does not, are nearer than twice that (and where they are
-//   equal), the wave does the token again in float64.
-// The largest of 64 lanes in six steps of data-parallel primitives, the expert by a ballot: the lowest index of equal ones.
+//   equal), float64 decides: a wave does its token again, a row of 16 lanes puts those chosen and the next one in order, one to a lane, and
+//   leaves to the wave a token with a group, or one more expert, in doubt.
+// The largest of 64 lanes in six steps of data-parallel primitives, the expert by a ballot (of 16 in four steps each): the lowest index of equal ones.
+//
+// 8192 tokens, 8 of 256 experts, sigmoid, bias, 4 of 8 groups: 12.2 us and 6.7 for the places; vector instructions issue in 56 and 58 % of the
+// clocks in which a compute unit has waves, the rest is waiting (a wave waits for half its life).
 //
 // The rows by expert: 32 tokens to a workgroup, a word of 32 bits for each expert with a bit for each token that has it.
 // A row's place among the workgroup's rows of its expert is the number of bits below its own, and the number of bits is
@@ -346,7 +351,9 @@ __device__ __forceinline__ bool route_row(const RouteArgs &P, int type, int64_t 
       c[i] = x[i] > NONE ? c[i] : NONE;
       size = c[i] > NONE ? __builtin_fmaxf(size, __builtin_fabsf(c[i])) : size;
     }
-    near = 2.0f * ((P.sigmoid ? 0x1p-22f : 0x1p-18f * over) + row_most(size) * 0x1p-24f);  // (as in route_token)
+    // As in route_token, but for the chain of softmax's sum: up to 31 additions in a lane and 4 over the row, 35 2^-24; the terms and their arguments
+    // 14 2^-24, the score's own argument, exponential, reciprocal and product below 6: 55 of the 64 2^-24 that 2^-18 are.
+    near = 2.0f * ((P.sigmoid ? 0x1p-22f : 0x1p-18f * over) + row_most(size) * 0x1p-24f);
   }
   lost = any_of_row(lost, lane);
   bool doubt = false;
@@ -361,7 +368,7 @@ __device__ __forceinline__ bool route_row(const RouteArgs &P, int type, int64_t 
       two = __builtin_fmaxf(__builtin_fmaxf(two, o2), __builtin_fminf(one, o1));
       one = __builtin_fmaxf(one, o1);
     };
-    // (lane ^ 1, ^ 2; then the other half of eight and of sixteen lanes, whose quarters have the same by now)
+    // (lane ^ 1, ^ 2; then the other half of eight lanes, whose quarters have the same by now: of more than one group none has 16 lanes)
     if (span > 1) join(moved<0xb1, 0xf>(one, one), moved<0xb1, 0xf>(two, two));
     if (span > 2) join(moved<0x4e, 0xf>(one, one), moved<0x4e, 0xf>(two, two));
     if (span > 4) join(moved<0x141, 0xf>(one, one), moved<0x141, 0xf>(two, two));
@@ -617,8 +624,11 @@ hipError_t launch_route(RouteArgs P, int type, void *ws, hipStream_t s) {
     P.counts = static_cast<uint8_t *>(ws);
     P.ranks = P.counts + counts_bytes(P.tokens, P.experts);
   }
-  // Four tokens to a wave (517 tokens, 60 experts 7.6 -> 5.1 us, 8192 and 256 12.3 -> 7.8), where the groups fit 16 lanes; up to 32 tokens one
-  // has a wave of its own, which is sooner done.
+  // Four tokens to a wave where the groups fit 16 lanes: without the places, 517 tokens, 4 of 60 experts, softmax 8.6 -> 3.9 us; 8192 tokens, 8 of
+  // 256 experts, softmax 14.7 -> 7.2, sigmoid and bias 18.3 -> 9.6, by groups as well 39.7 -> 12.9.  Up to 32 tokens a token has a wave of its own,
+  // and the rows by expert are put in place by the same launch, which the form of four leaves to a second one.  With the places, 8 of 128 experts,
+  // softmax, tokens 8, 16, 32 and 33 (the first in two launches): 6.0, 7.8, 12.8, 9.8 us; 8 of 256, sigmoid, bias, 4 of 8 groups: 13.0, 18.8, 33.9,
+  // 14.2.  So it is the sooner done up to some 20 tokens without groups and 8 with them; from there to 32 it is not, and the limit is what 32 bits hold.
   int per = P.experts <= 64 ? 1 : P.experts <= 128 ? 2 : P.experts <= 256 ? 4 : P.experts <= 512 ? 8 : 16;
   bool four = P.tokens > TOKENS && per <= 8 && P.top <= 15;
   if (four) {
