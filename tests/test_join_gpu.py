@@ -389,3 +389,24 @@ def test_scales_of_rows_next_to_the_smallest_numbers(gpu, kind, cols, rows):
     torch.cuda.synchronize()
     assert torch.equal(q[:, :cols], Q[:, :cols])
     assert ((other[:-1].double() - s[:-1].double()).abs() <= 60 * U * s[:-1]).all()
+
+
+@pytest.mark.parametrize("cols", [100, 4096])
+def test_offsets_of_rows_that_pass_31_and_32_bits(gpu, cols):
+    """Three rows 2^30 and 2^31 - 1 elements apart, in every operand at once, against the same rows side by side."""
+    import torch
+    rows = 3
+    case = Case(rows, cols, 2, BF16, RMS, RMS, gate_rows=1, seed=19)
+    near = case.call(gpu)
+    weights = [x.cuda() for x in (case.pw, case.nw, case.w)]
+    for lead in (2 ** 30, 2 ** 31 - 1):
+        far = lambda x, n, kind=torch.bfloat16: torch.as_strided(torch.empty((n - 1) * lead + cols, dtype=kind, device="cuda"), (n, cols), (lead, 1)).copy_(x)  # noqa: E731
+        X, G, Rd = far(case.X, rows * 2), far(case.G, rows), far(case.R_, rows)
+        H, N, Q = far(torch.zeros(rows, cols), rows), far(torch.zeros(rows, cols), rows), far(torch.zeros(rows, cols), rows, torch.int8)
+        s = torch.zeros(rows, device="cuda")
+        gpu.mipgemm_join_rows(rows, cols, 2, BF16, X, lead, rows * 2, case.places.cuda(), weights[2], RMS, weights[0], None, G, lead, 1, 1.0, Rd, lead, H, lead,
+                              RMS, weights[1], None, EPS, N, lead, Q, lead, s)
+        torch.cuda.synchronize()
+        for got, want in zip((H, N, Q, s), near):
+            assert torch.equal(got, want[:rows, :cols] if want.dim() > 1 else want[:rows]), lead
+        del X, G, Rd, H, N, Q

@@ -304,3 +304,22 @@ def test_weights_far_below_the_largest(gpu, tokens, experts):
         _check(gpu, x, F32, 6, sigmoid=True, normalise=normalise)
         _check(gpu, x, F32, 6, sigmoid=True, normalise=normalise, bias=torch.zeros(experts))
         _check(gpu, x, F32, 6, sigmoid=True, normalise=normalise, groups=2, top_groups=2, best=2, scale=2.5)
+
+
+@pytest.mark.parametrize("tokens", [3, 40])
+@pytest.mark.parametrize("kind", [F32, BF16])
+def test_offsets_of_tokens_that_pass_31_and_32_bits(gpu, tokens, kind):
+    import torch
+    experts, top = 70, 5
+    x = _normal(tokens, experts, seed=21)
+    near = _route(gpu, x, kind, top, sigmoid=True)
+    for lead in (2 ** 27 + 1, 2 ** 31 - 1):
+        if tokens * lead > 2 ** 34:  # (64 GB of float32)
+            continue
+        far = torch.as_strided(torch.empty((tokens - 1) * lead + experts, dtype=R.TORCH[kind], device="cuda"), (tokens, experts), (lead, 1))
+        far.copy_(x)
+        ids, w = torch.zeros((tokens, top), dtype=torch.int32, device="cuda"), torch.zeros((tokens, top), device="cuda")
+        gpu.mipgemm_route(tokens, experts, top, far, lead, kind, None, 1, 1, 1, 1, 1, 1.0, ids, w)
+        torch.cuda.synchronize()
+        assert np.array_equal(ids.cpu().numpy(), near[0]) and np.array_equal(w.cpu().numpy(), near[1]), lead
+        del far
